@@ -1,16 +1,16 @@
 // Matrix product in 8-bit floating point with a power-of-two scale for every 128 values along the contraction
-// (rampde_fp8_quantize, rampde_fp8_matmul).
+// (rampde_fp8_quantize, rampde_fp8_matmul, rampde_fp8_matmul_short).
 //
-// gfx950's scaled matrix instructions multiply 8-bit values and apply an exponent per operand row and 32 values in the instruction,
-// so a block scale that is a power of two costs nothing.  All products and sums of a block of C stay in fp32 accumulators.
+// Sums in fp32 (rampde_fp8_matmul, any result): every e4m3 value times its scale is a bf16 number, one instruction converts two of
+// them, and 16-bit matrix instructions form exact products and fp32 sums (5e-9 relative on blocks of 128 normally distributed values
+// against 64 bits, 8e-8 on values spread over all exponents).
 //
-// Precision.  The 8-bit matrix instructions (scaled or not) align 8 products that follow one another along the contraction to the
-// largest of them and drop what is more than 13 binary places below its leading one; from one such group to the next, and to the
-// accumulator, they keep 24 bits.  A sum of eight is off by at most 7 * 2^-13 of its largest product; measured on blocks of 128
-// against 64 bits, 1.5e-5 relative for normally distributed values, 4.9e-5 for values spread over all exponents.  Results of 16 bits
-// round at 2e-4 (f16) or 2e-3 (bf16), an order above that, and take them.  An fp32 result (a weight gradient, which is summed on over
-// batches) takes 16-bit matrix instructions instead: every e4m3 value times its scale is a bf16 number, one instruction converts two
-// of them, products are exact and sums are fp32 (5e-9 and 8e-8 on the same blocks), at half the rate.
+// Short sums (rampde_fp8_matmul_short, results of 16 bits; a caller has to ask for them): gfx950's scaled matrix instructions multiply
+// the 8-bit values and apply an exponent per operand row and 32 values, so that a scale that is a power of two costs nothing, at twice
+// the rate.  They (scaled or not) align 8 products that follow one another along the contraction to the largest of them and drop what
+// is more than 13 binary places below its leading one; from one such group to the next, and to the accumulator, they keep 24 bits.  A
+// sum of eight is off by at most 7 * 2^-13 of its largest product: 1.5e-5 and 4.9e-5 on the same blocks, which flips the rounding of
+// enough results that they differ from those of fp32 sums by 1e-4 to 3e-4 norm-wise.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -296,7 +296,7 @@ __device__ inline void put_c(const Fp8Args& g, int64_t m, int64_t n, f32x4 v) {
 // neighbouring columns of a row of C.  A wavefront's load touches 16 rows, a line of each, and that, not the latency, is what bounds
 // it: 4 blocks requested at a time took as long.  In cache, 16 x 4096 x 4096 takes 8 us (2.1 TB/s of B), 16 x 4096 x 2048 5 us.
 constexpr int kFewWaves = 16;
-template <class T, int FM>
+template <class T, bool SHORT, int FM>
 __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_rows(Fp8Args g) {
   constexpr int AHEAD = 2;
   __shared__ f32x4 sums[kFewWaves][FM][64];
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_rows(Fp8Args g) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       if (k + u >= k1) break;
-      if constexpr (std::is_same<T, F32>::value) {
+      if constexpr (!SHORT) {
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           const u16x8 wb = to_bf16(fb[u][2 * h], fb[u][2 * h + 1], scale_value(sb[u]));
@@ -376,11 +376,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_rows(Fp8Args g) {
 // are read while the first is multiplied, which frees the slot, and those of the next block's first half while the second is; a block
 // has the time of a whole one to arrive.
 //
-// 256 x 256 on 8 wavefronts (2 x 4, each 128 x 64): per block of 128, reading fragments from LDS takes as many cycles as the matrix
-// instructions (about 2000 at their full rates), and the chip's power lets matrix instructions on such data run at 3.2 to 3.7
-// PFLOP/s (5 on constant data).  Measured: 16384 x 4096 x 2048 122 to 151 us and 16384 x 2048 x 4096 120 to 154 us by card and heat
-// (1.8 to 2.3 PFLOP/s); fp32 results 4096 x 2048 x 16384 224 to 275 us (1.0 to 1.2 of the 1.8 PFLOP/s that 16-bit instructions reach by
-// themselves).  Tried and slower or no faster: 4 wavefronts of 128 x 128, rings of 3 to 5 half-size slots, tiles of 256 x 128, the 16 x 16
+// 256 x 256 on 8 wavefronts (2 x 4, each 128 x 64).  Sums in fp32 are bound by the 16-bit matrix instructions and the conversions in
+// front of them: bf16 results 16384 x 4096 x 2048 211 us and 16384 x 2048 x 4096 203 us, fp32 results 4096 x 2048 x 16384 224 to 275 us by
+// card and heat (1.0 to 1.35 of the 1.8 PFLOP/s that these instructions reach by themselves).  Short sums: per block of 128, reading
+// fragments from LDS takes as many cycles as the matrix instructions (about 2000 at their full rates), and the chip's power lets matrix
+// instructions on such data run at 3.2 to 3.7 PFLOP/s (5 on constant data); the same two products 122 to 151 and 119 to 154 us (1.8 to
+// 2.3 PFLOP/s).  Tried and slower or no faster: 4 wavefronts of 128 x 128, rings of 3 to 5 half-size slots, tiles of 256 x 128, the 16 x 16
 // instructions (15 % faster by themselves, but their fragments spill here), wave priorities, conversions a group ahead.
 template <int WM, int WN, int FM, int FN>
 struct Fp8Tile {
@@ -399,10 +400,9 @@ __device__ inline void load_to_lds(const uint8_t* from, __attribute__((address_s
   __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-template <class T, int WM, int WN, int FM, int FN>
+template <class T, bool SHORT, int WM, int WN, int FM, int FN>
 __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp8Args g) {
   typedef Fp8Tile<WM, WN, FM, FN> P;
-  constexpr bool EXACT = std::is_same<T, F32>::value;  // 16-bit matrix instructions (see above)
   typedef __attribute__((address_space(3))) uint8_t lds_u8;
   extern __shared__ __attribute__((aligned(16))) uint8_t fp8_smem[];
   lds_u8* ring = (lds_u8*)fp8_smem;
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[a][b][q] = 0.f;
   auto multiply = [&](const i32x8 (&fa)[FM], const i32x8 (&fb)[FN]) {
-    if constexpr (EXACT) {
+    if constexpr (!SHORT) {
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         u16x8 wa[FM], wb[FN];
@@ -517,11 +517,11 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp
 
   // reads, requests and arithmetic of half a block go out between its matrix instructions, in whose shadow they then are
   auto spread = [&](auto requests) {
-    if constexpr (EXACT) {
+    if constexpr (!SHORT) {
       __builtin_amdgcn_sched_barrier(0);
       return;
     }
-    constexpr int NM = (EXACT ? 4 : 1) * FM * FN, READS = 2 * (FM + FN), EACH = (READS + NM - 1) / NM;
+    constexpr int NM = FM * FN, READS = 2 * (FM + FN), EACH = (READS + NM - 1) / NM;
 #pragma unroll
     for (int i = 0; i < NM; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);     // a matrix instruction
@@ -598,7 +598,7 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp
     }
     return;
   }
-  if constexpr (EXACT) {
+  if constexpr (std::is_same<T, F32>::value) {
 #pragma unroll
     for (int a = 0; a < FM; ++a) {
       const int64_t m = m0 + (wm * FM + a) * 32 + frow;
@@ -697,15 +697,56 @@ int launch_kernel(Kern kern, const Fp8Args& g, unsigned threads, size_t lds, hip
   HIP_TRY(hipGetLastError());
   return RAMPDE_OK;
 }
-template <class T, int WM, int WN, int FM, int FN>
+template <class T, bool SHORT, int WM, int WN, int FM, int FN>
 int launch_tiles(Fp8Args& g, hipStream_t st) {
   typedef Fp8Tile<WM, WN, FM, FN> P;
   g.tiles_m = (int)((g.M + P::TM - 1) / P::TM);
   g.tiles_n = (int)((g.N + P::TN - 1) / P::TN);
-  return launch_kernel(fp8_tile<T, WM, WN, FM, FN>, g, 64 * P::WAVES, P::LDS, st);
+  return launch_kernel(fp8_tile<T, SHORT, WM, WN, FM, FN>, g, 64 * P::WAVES, P::LDS, st);
 }
 
 bool sizes_ok(int64_t R, int64_t K) { return R >= 1 && K >= 1 && R < (int64_t)1 << 31 && K < (int64_t)1 << 31; }
+
+size_t product_space(int64_t M, int64_t N, const Fp8Plan& p) { return 256 + (p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0); }
+
+int check_product(int64_t M, int64_t N, int64_t K, const void* a_values, const void* a_scales, const void* b_values, const void* b_scales,
+                  rampde_dtype c_type, int accumulate, void* C, int64_t ldc, void* workspace, size_t workspace_bytes, Fp8Args& g, Fp8Plan& p) {
+  if (!sizes_ok(M, K) || !sizes_ok(N, K) || !known_type(c_type) || !a_values || !a_scales || !b_values || !b_scales || !C) return RAMPDE_EINVAL;
+  if (accumulate && c_type != RAMPDE_F32) return RAMPDE_EINVAL;
+  if (ldc == 0) ldc = N;
+  if (ldc < N || ldc >= (int64_t)1 << 40 || ldc > ((int64_t)1 << 46) / M || !aligned_to(a_values, 16) || !aligned_to(a_scales, 16) || !aligned_to(b_values, 16) ||
+      !aligned_to(b_scales, 16) || !aligned_to(C, type_size(c_type)))
+    return RAMPDE_EINVAL;
+  p = fp8_plan(M, N, K);
+  if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < product_space(M, N, p)) return RAMPDE_EWORKSPACE;
+  if (((M + 127) / 128) * ((N + 127) / 128) >= (int64_t)1 << 30) return RAMPDE_EUNSUPPORTED;
+  if (K >= (int64_t)1 << 23) return RAMPDE_EUNSUPPORTED;  // (offsets of a tile's rows fit 32 bits)
+  g.a = (const uint8_t*)a_values, g.sa = (const uint8_t*)a_scales, g.b = (const uint8_t*)b_values, g.sb = (const uint8_t*)b_scales;
+  g.c = C, g.M = M, g.N = N, g.ldc = ldc, g.accumulate = accumulate != 0;
+  g.Kq = round_up(K, 128), g.nb = (int)(g.Kq / 128), g.Ks = round_up(g.nb, 4);
+  g.vec = aligned_to(C, 16) && ldc * (int64_t)type_size(c_type) % 16 == 0;
+  g.splits = p.splits, g.split_blocks = p.split_blocks, g.part = (float*)workspace;
+  return RAMPDE_OK;
+}
+
+template <class T, bool SHORT>
+int multiply(Fp8Args& g, const Fp8Plan& p, hipStream_t st) {
+  if (p.kind == kFewRows) {
+    const dim3 grid((unsigned)((g.N + 15) / 16), (unsigned)g.splits);
+    if (g.M <= 16) fp8_few_rows<T, SHORT, 1><<<grid, 64 * kFewWaves, 0, st>>>(g);
+    else fp8_few_rows<T, SHORT, 2><<<grid, 64 * kFewWaves, 0, st>>>(g);
+    HIP_TRY(hipGetLastError());
+  } else if (p.kind == kLargeTiles) {
+    if (const int rc = launch_tiles<T, SHORT, 2, 4, 4, 2>(g, st)) return rc;
+  } else {
+    if (const int rc = launch_tiles<T, SHORT, 2, 2, 2, 2>(g, st)) return rc;
+  }
+  if (g.splits > 1) {
+    fp8_fold<T><<<(unsigned)std::min<int64_t>((g.M * g.N + 255) / 256, 4096), 256, 0, st>>>(g);
+    HIP_TRY(hipGetLastError());
+  }
+  return RAMPDE_OK;
+}
 
 }  // namespace
 }  // namespace rampde
@@ -760,48 +801,27 @@ int rampde_fp8_quantize(rampde_dtype src_type, rampde_fp8_mode mode, int64_t R, 
 
 size_t rampde_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   if (!sizes_ok(M, K) || !sizes_ok(N, K)) return 0;
-  const Fp8Plan p = fp8_plan(M, N, K);
-  return 256 + (p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0);
+  return product_space(M, N, fp8_plan(M, N, K));
 }
 
 int rampde_fp8_matmul(int64_t M, int64_t N, int64_t K, const void* a_values, const void* a_scales, const void* b_values,
                       const void* b_scales, rampde_dtype c_type, int accumulate, void* C, int64_t ldc, void* workspace,
                       size_t workspace_bytes, void* hip_stream) {
-  if (!sizes_ok(M, K) || !sizes_ok(N, K) || !known_type(c_type) || !a_values || !a_scales || !b_values || !b_scales || !C) return RAMPDE_EINVAL;
-  if (accumulate && c_type != RAMPDE_F32) return RAMPDE_EINVAL;
-  if (ldc == 0) ldc = N;
-  if (ldc < N || ldc >= (int64_t)1 << 40 || ldc > ((int64_t)1 << 46) / M || !aligned_to(a_values, 16) || !aligned_to(a_scales, 16) || !aligned_to(b_values, 16) ||
-      !aligned_to(b_scales, 16) || !aligned_to(C, type_size(c_type)))
-    return RAMPDE_EINVAL;
-  if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < rampde_fp8_workspace_bytes(M, N, K)) return RAMPDE_EWORKSPACE;
-  if (((M + 127) / 128) * ((N + 127) / 128) >= (int64_t)1 << 30) return RAMPDE_EUNSUPPORTED;
-  if (K >= (int64_t)1 << 23) return RAMPDE_EUNSUPPORTED;  // (offsets of a tile's rows fit 32 bits)
   Fp8Args g{};
-  g.a = (const uint8_t*)a_values, g.sa = (const uint8_t*)a_scales, g.b = (const uint8_t*)b_values, g.sb = (const uint8_t*)b_scales;
-  g.c = C, g.M = M, g.N = N, g.ldc = ldc, g.accumulate = accumulate != 0;
-  g.Kq = round_up(K, 128), g.nb = (int)(g.Kq / 128), g.Ks = round_up(g.nb, 4);
-  g.vec = aligned_to(C, 16) && ldc * (int64_t)type_size(c_type) % 16 == 0;
-  const Fp8Plan p = fp8_plan(M, N, K);
-  g.splits = p.splits, g.split_blocks = p.split_blocks, g.part = (float*)workspace;
-  const hipStream_t st = (hipStream_t)hip_stream;
-  return by_type(c_type, [&](auto tag) {
-    typedef decltype(tag) T;
-    if (p.kind == kFewRows) {
-      const dim3 grid((unsigned)((N + 15) / 16), (unsigned)g.splits);
-      if (M <= 16) fp8_few_rows<T, 1><<<grid, 64 * kFewWaves, 0, st>>>(g);
-      else fp8_few_rows<T, 2><<<grid, 64 * kFewWaves, 0, st>>>(g);
-      HIP_TRY(hipGetLastError());
-    } else if (p.kind == kLargeTiles) {
-      if (const int rc = launch_tiles<T, 2, 4, 4, 2>(g, st)) return rc;
-    } else {
-      if (const int rc = launch_tiles<T, 2, 2, 2, 2>(g, st)) return rc;
-    }
-    if (g.splits > 1) {
-      fp8_fold<T><<<(unsigned)std::min<int64_t>((M * N + 255) / 256, 4096), 256, 0, st>>>(g);
-      HIP_TRY(hipGetLastError());
-    }
-    return (int)RAMPDE_OK;
-  });
+  Fp8Plan p;
+  if (const int rc = check_product(M, N, K, a_values, a_scales, b_values, b_scales, c_type, accumulate, C, ldc, workspace, workspace_bytes, g, p))
+    return rc;
+  return by_type(c_type, [&](auto tag) { return multiply<decltype(tag), false>(g, p, (hipStream_t)hip_stream); });
+}
+
+int rampde_fp8_matmul_short(int64_t M, int64_t N, int64_t K, const void* a_values, const void* a_scales, const void* b_values,
+                            const void* b_scales, rampde_dtype c_type, void* C, int64_t ldc, void* workspace,
+                            size_t workspace_bytes, void* hip_stream) {
+  if (c_type == RAMPDE_F32) return RAMPDE_EINVAL;  // (it would hold places that the sums do not have)
+  Fp8Args g{};
+  Fp8Plan p;
+  if (const int rc = check_product(M, N, K, a_values, a_scales, b_values, b_scales, c_type, 0, C, ldc, workspace, workspace_bytes, g, p)) return rc;
+  return c_type == RAMPDE_F16 ? multiply<F16, true>(g, p, (hipStream_t)hip_stream) : multiply<BF16, true>(g, p, (hipStream_t)hip_stream);
 }
 
 }  // extern "C"
