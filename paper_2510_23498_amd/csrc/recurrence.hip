@@ -201,16 +201,17 @@ struct Rows {
 };
 
 // ---- What tiles tell one another.  A chain's tiles are numbered as it runs, and go in windows of kWindow.  A tile has one word per
-// channel, all ones until it has something to say.  Tiles but a window's last say {A, U}: they take a state h to A h + U (A is a
-// product of factors 1 - r in [0, 1], or a NaN).  A window's last says {0, H}: the state behind it.  The state in front of a tile is
-// that behind the window before, taken through the window's tiles one after the other: what is added to what does not depend on
-// who was first, and two calls give the same bits.  A word is written once and read as a whole (64-bit atomics of device scope), so
-// nothing depends on the order of other stores.  A chain advances by a window in 1.5 us: one alone over 65536 steps takes 49 us, which
+// channel, all ones until it has something to say.  A chain's first tile and every window's last say {0, H}: the state behind them.
+// The others say {A, U}: they take a state h to A h + U (A is a product of factors 1 - r in [0, 1], or a NaN).  The state in front of a
+// tile is that behind the window before (the first tile), taken through the window's tiles one after the other: what is added to what
+// does not depend on who was first, and two calls give the same bits.  A word is written once and read as a whole (64-bit atomics of
+// device scope), so nothing depends on the order of other stores.  The first tile alone reads the state that the caller gives, and its
+// word is made of what it read: the last tile, whose state is made of that word, may write over it (hT = h0, dh0 = dhT).  A chain advances by a window in 1.5 us: one alone over 65536 steps takes 49 us, which
 // windows of 32 tiles shorten to 39 while 8 x 4096 x 2048 goes from 95 to 100 us.
 //
 // Every wait ends: a workgroup draws its tile by a ticket of its chain (block of channels), in the order of the chain, so that the
-// workgroups it waits for have drawn theirs before and are running; tiles say {A, U} before they wait, and a window's last waits for
-// tiles before it alone.  (One ticket for all chains: the draws of 512 workgroups then follow one another, 17 instead of 13 us for
+// workgroups it waits for have drawn theirs before and are running; the first tile waits for none, tiles say {A, U} before they wait,
+// and a window's last waits for tiles before it alone.  (One ticket for all chains: the draws of 512 workgroups then follow one another, 17 instead of 13 us for
 // 7 x 1003 x 1024.)
 __device__ inline uint64_t word_of(float a, float u) {
   if (a != a) a = NAN;  // (not the pattern of an empty word)
@@ -398,6 +399,11 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(typename Elem<T>::S) == 2 && RE
   const f32x2 none = {0.f, 0.f};
   f32x2 cur, A = {1.f, 1.f}, U = {0.f, 0.f};
   const bool ends_window = (tile & (kWindow - 1)) == kWindow - 1, chained = tile + 1 < g.tiles;
+  f32x2 h = none;  // the state in front of the tile
+  if (wave == 0 && tile == 0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) h[i] = g.h0 && l.live(i) ? g.h0[l.c(i)] : 0.f;
+  }
   if (wave == 0 && chained) {
     for (int s = 0; s < waves; ++s) {
       const f32x4 v = seg[s][lane];
@@ -407,19 +413,15 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(typename Elem<T>::S) == 2 && RE
         A[i] *= v[2 * i];
       }
     }
-    if (!ends_window) publish(g, l, block, tile, A, U);
+    if (tile == 0) publish(g, l, block, tile, none, f32x2{fmaf(A[0], h[0], U[0]), fmaf(A[1], h[1], U[1])});
+    else if (!ends_window) publish(g, l, block, tile, A, U);
   }
   if (tile > 0) {
     gather_words(g, l, block, tile, wave, said);
     __syncthreads();
   }
   if (wave == 0) {
-    f32x2 h = none;
-    if (tile < kWindow) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) h[i] = g.h0 && l.live(i) ? g.h0[l.c(i)] : 0.f;
-    }
-    h = taken_through(said, tile - first_word(tile), h);
+    if (tile > 0) h = taken_through(said, tile - first_word(tile), none);
     if (chained && ends_window) publish(g, l, block, tile, none, f32x2{fmaf(A[0], h[0], U[0]), fmaf(A[1], h[1], U[1])});
     start[lane] = h;
   }
@@ -556,6 +558,11 @@ __global__ __launch_bounds__(64 * kWaves, REACH == kPairs ? 4 : 1) void recurren
   const f32x2 none = {0.f, 0.f};
   f32x2 A = {1.f, 1.f}, U = {0.f, 0.f};
   const bool ends_window = (place & (kWindow - 1)) == kWindow - 1, chained = tile > 0;
+  f32x2 h = none;  // what comes to the tile from the steps behind it
+  if (wave == 0 && place == 0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) h[i] = g.hT && l.live(i) ? g.hT[l.c(i)] : 0.f;
+  }
   if (wave == 0 && chained) {
     for (int s = waves - 1; s >= 0; --s) {
       const f32x4 v = seg[s][lane];
@@ -565,19 +572,15 @@ __global__ __launch_bounds__(64 * kWaves, REACH == kPairs ? 4 : 1) void recurren
         A[i] *= v[2 * i];
       }
     }
-    if (!ends_window) publish(g, l, block, place, A, U);
+    if (place == 0) publish(g, l, block, place, none, f32x2{fmaf(A[0], h[0], U[0]), fmaf(A[1], h[1], U[1])});
+    else if (!ends_window) publish(g, l, block, place, A, U);
   }
   if (place > 0) {
     gather_words(g, l, block, place, wave, said);
     __syncthreads();
   }
   if (wave == 0) {
-    f32x2 h = none;
-    if (place < kWindow) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) h[i] = g.hT && l.live(i) ? g.hT[l.c(i)] : 0.f;
-    }
-    h = taken_through(said, place - first_word(place), h);
+    if (place > 0) h = taken_through(said, place - first_word(place), none);
     if (chained && ends_window) publish(g, l, block, place, none, f32x2{fmaf(A[0], h[0], U[0]), fmaf(A[1], h[1], U[1])});
     start[lane] = h;
   }
