@@ -86,9 +86,16 @@ __device__ inline void store8(typename Elem<T>::S* p, int n, const float (&f)[8]
   }
 }
 
-// 1 / (1 + exp(-z)) on the hardware exp2 and reciprocal (relative error about 2e-7; 0 where the exponential overflows)
-__device__ inline float logistic(float z) {
-  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f));
+// s = 1 / (1 + exp(-z)) on the hardware exp2 and reciprocal (relative error about 2e-7; 0 where the exponential overflows), and
+// 1 - s to as many places: by subtraction, that of an open gate has lost 12 of 24 at z = 8 and all of them at 17.
+struct Gate {
+  float s, c;
+  bool open;  // s > 1/2
+};
+__device__ inline Gate gate_of(float z) {
+  const float e = __builtin_amdgcn_exp2f(z * -1.44269504088896341f), s = __builtin_amdgcn_rcpf(1.f + e);
+  return {s, e < 1.f ? e * s : 1.f - s, e < 1.f};
 }
+__device__ inline float logistic(float z) { return gate_of(z).s; }
 
 }  // namespace rampde

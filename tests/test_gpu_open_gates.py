@@ -1,0 +1,104 @@
+"""Gates far from zero: 1 - s(z) of an open gate is known to as many places as s(z) of a closed one.
+
+Tolerances, element by element and relative: exp(-z) is off by the rounding of its argument, |z| 2^-24, and one unit of the hardware's
+exponential, the reciprocal by another, and a step has a handful of roundings: (16 + 2 |z|) 2^-24 for a step's factor, that many times for
+a product of factors; and the rounding to the result's type (f16: 2^-25 absolutely among subnormal numbers)."""
+import numpy as np
+import pytest
+
+import sequence_reference as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+LOW = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+TINY = {"bf16": 0.0, "f16": 2.0 ** -24, "f32": 2.0 ** -126}
+GATES = (0.0, 0.5, 2.0, 4.0, 8.0, 11.0, 14.0, 17.0, 20.0, 40.0)
+
+
+@pytest.fixture(scope="module")
+def rb():
+    from paper_2510_23498_amd import binding
+    binding.load_library()
+    return binding
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _near(got, want, low, steps, z, name):
+    got, want = _np(got), np.asarray(want)
+    off = np.abs(got - want)
+    bound = (ref.UNIT[low] + steps * (16 + 2 * np.abs(z)) * 2.0 ** -24) * np.abs(want) + TINY[low]
+    assert (off <= bound).all(), f"{name}: {(off / np.maximum(np.abs(want), 1e-300)).max():.3e} off"
+
+
+def _channels(B, T, D, share, z):
+    """Gates z, -z of channels in turn"""
+    gates = torch.tensor([z, -z] * (D // share))[:D // share]
+    return gates.expand(B, T, D // share).contiguous(), np.repeat(gates.numpy().astype(np.float64), share)
+
+
+@pytest.mark.parametrize("z", GATES)
+@pytest.mark.parametrize("low", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("share", [1, 2, 16])
+def test_gradients_of_one_step(rb, low, z, share):
+    B, D = 3, 64
+    rng = np.random.default_rng(int(8 * z) + share)
+    g = lambda *s: torch.from_numpy(rng.uniform(0.5, 1.5, s).astype(np.float32))  # noqa: E731
+    zt, zn = _channels(B, 1, D, share, z)
+    x, dh = g(B, 1, D).to(LOW[low]).cuda(), g(B, 1, D).to(LOW[low]).cuda()
+    h0, dhT, zt = -g(B, D).cuda(), g(B, D).cuda(), zt.to(LOW[low]).cuda()   # (all terms of one sign: nothing cancels)
+    h, hT, states = rb.rampde_recurrence_fwd(x, zt, h0=h0, save_states=True)
+    dx, dz, dh0 = rb.rampde_recurrence_bwd(x, zt, states, dh, dhT=dhT, h0=h0)
+    wh, wT, wdx, wdz, wdh0 = ref.recurrence(_np(x), _np(zt), _np(h0), None, _np(dh), _np(dhT))
+    if share == 1:   # (1 - s subtracts in the reference too, which 64 bits leave room for up to z = 20)
+        s, c = 1 / (1 + np.exp(-zn)), 1 / (1 + np.exp(zn))
+        G = _np(dh)[:, 0] + _np(dhT)
+        wdz, wdh0 = (G * (_np(x)[:, 0] - _np(h0)) * s * c)[:, None], G * c
+    _near(dx, wdx, low, 1, z, "dx")
+    if share == 1 or z <= 20:
+        _near(dz, wdz, low, 1, z, "dz")
+        _near(dh0, wdh0, "f32", 1, z, "dh0")
+
+
+@pytest.mark.parametrize("z", [2.0, 4.0, 8.0])
+@pytest.mark.parametrize("D", [128, 63])
+def test_what_open_gates_leave_of_the_last_gradient(rb, z, D):
+    """No gradient but the last one's: products of 1 - s over the steps, fp32 (inputs of alternating signs, so that x - h is large)"""
+    T = 9
+    x = (torch.tensor([1.5, -1.5] * 5)[:T, None] * torch.ones(2, T, D)).cuda()
+    zt, h0 = torch.full((2, T, D), z, device="cuda"), torch.full((2, D), -1.0, device="cuda")
+    dhT = torch.full((2, D), 3.0, device="cuda")
+    states = rb.rampde_recurrence_fwd(x, zt, h0=h0, save_states=True)[2]
+    dx, dz, dh0 = rb.rampde_recurrence_bwd(x, zt, states, None, dhT=dhT, h0=h0)
+    c, s = 1 / (1 + np.exp(z)), 1 / (1 + np.exp(-z))
+    G = 3 * c ** np.arange(T - 1, -1, -1)[None, :, None] * np.ones((2, T, D))
+    h = ref.recurrence(_np(x), _np(zt), _np(h0))[0]
+    before = np.concatenate([_np(h0)[:, None], h[:, :-1]], 1)
+    _near(dx, G * s, "f32", T, z, "dx")
+    _near(dh0, 3 * c ** T * np.ones((2, D)), "f32", T, z, "dh0")
+    _near(dz, G * (_np(x) - before) * s * c, "f32", T + 2, z, "dz")
+
+
+@pytest.mark.parametrize("T", [40, 300, 2500])
+@pytest.mark.parametrize("low", ["bf16", "f16", "f32"])
+def test_gradients_of_open_gates_along_a_sequence(rb, low, T):
+    """Inputs of alternating signs (so that x - h does not cancel) and gradients of one sign, gates of 6 to 16, several tiles"""
+    B, D = 2, 130
+    rng = np.random.default_rng(T)
+    sign = torch.tensor([1.0, -1.0] * ((T + 1) // 2))[:T, None]
+    x = (torch.from_numpy(rng.uniform(1, 2, (B, T, D)).astype(np.float32)) * sign).to(LOW[low]).cuda()
+    z = torch.from_numpy(rng.uniform(6, 16, (B, T, D)).astype(np.float32)).to(LOW[low]).cuda()
+    dh = torch.from_numpy(rng.uniform(0.5, 1.5, (B, T, D)).astype(np.float32)).to(LOW[low]).cuda()
+    h0 = torch.full((B, D), -1.0, device="cuda")
+    h, hT, states = rb.rampde_recurrence_fwd(x, z, h0=h0, save_states=True)
+    dx, dz, dh0 = rb.rampde_recurrence_bwd(x, z, states, dh, h0=h0)
+    zn, xn = _np(z), _np(x)
+    want = ref.recurrence(xn, zn, _np(h0), None, _np(dh))
+    # (the reference's 1 - s is off by 2^-53 exp(16), 1e-9, relatively)
+    _near(h, want[0], low, 2, zn, "h")
+    _near(dx, want[2], low, 2, zn, "dx")
+    _near(dz, want[3], low, 4, zn, "dz")
+    _near(dh0, want[4], "f32", 2, 16.0, "dh0")
