@@ -86,15 +86,14 @@ __device__ inline void store8(typename Elem<T>::S* p, int n, const float (&f)[8]
   }
 }
 
-// s = 1 / (1 + exp(-z)) on the hardware exp2 and reciprocal (relative error about 2e-7; 0 where the exponential overflows), and
-// 1 - s to as many places: by subtraction, that of an open gate has lost 12 of 24 at z = 8 and all of them at 17.
+// e = exp(-z) and s = 1 / (1 + e) on the hardware exp2 and reciprocal (relative error about 2e-7; s is 0 where e overflows).  1 - s is
+// e s, to as many places: by subtraction, that of an open gate has lost 12 of 24 at z = 8 and all of them at 17.
 struct Gate {
-  float s, c;
-  bool open;  // s > 1/2
+  float e, s;
 };
 __device__ inline Gate gate_of(float z) {
-  const float e = __builtin_amdgcn_exp2f(z * -1.44269504088896341f), s = __builtin_amdgcn_rcpf(1.f + e);
-  return {s, e < 1.f ? e * s : 1.f - s, e < 1.f};
+  const float e = __builtin_amdgcn_exp2f(z * -1.44269504088896341f);
+  return {e, __builtin_amdgcn_rcpf(1.f + e)};
 }
 __device__ inline float logistic(float z) { return gate_of(z).s; }
 

@@ -261,14 +261,15 @@ __global__ __launch_bounds__(64 * W * R, sizeof(typename Elem<T>::S) == 2 ? 4 : 
           unpack8<T>(gr[j], gt);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float gv = g.gate ? logistic(gt[i]) : 1.f;
+            const Gate v = gate_of(gt[i]);
+            const float gv = g.gate ? v.s : 1.f;
             nb[j][i] *= r_post;
             const float da = g.m.drop ? g.alpha * dv[j][i] * k[i] : g.alpha * dv[j][i];  // of s(gate) scale N(b) w_post
             const float dn = da * gv * sc[i];                                            // of N(b) w_post
             cs[0][j][i] = fmaf(dn, nb[j][i], cs[0][j][i]);
             cs[1][j][i] = fmaf(da * gv, nb[j][i] * wp[i], cs[1][j][i]);
             u[j][i] = dn * wp[i];
-            dg[i] = u[j][i] * nb[j][i] * (1.f - gv);
+            dg[i] = u[j][i] * nb[j][i] * (fminf(v.e, 0x1p126f) * v.s);  // (1 - s; where e overflows s is 0, and so is u)
             s1 = fmaf(u[j][i], nb[j][i], s1);
           }
           if (g.dgate) store8<T>((S*)g.dgate + row * g.ld_gate + c, WHOLE ? 8 : g.cols - c, dg);

@@ -483,7 +483,7 @@ __device__ inline float gate_sum(float a, float b, uint32_t share) {
 // A rate as one number that holds the smaller of r and 1 - r to fp32: r, or -(1 - r) for open gates (the sign says which, also of a
 // zero).  The backward pass multiplies by both: what an open gate leaves of a gradient is G (1 - r), not what G - G r leaves of it.
 // (Two numbers would take 32 registers more, and spill: 286 instead of 133 us for 8 x 4096 x 2048.)
-__device__ inline float rate_of(const Gate& v) { return v.open ? -v.c : v.s; }
+__device__ inline float rate_of(const Gate& v) { return v.e < 1.f ? -(v.e * v.s) : v.s; }
 __device__ inline bool is_open(float rate) { return __builtin_bit_cast(int, rate) < 0; }
 // (1 - r) v and r v.  (Closed: one rounding, of the difference.  A rounded 1 - r would be off the same way at every step.)
 __device__ inline float held(float rate, float v) { return fmaf(-rate, v, is_open(rate) ? 0.f : v); }

@@ -102,3 +102,31 @@ def test_gradients_of_open_gates_along_a_sequence(rb, low, T):
     _near(dx, want[2], low, 2, zn, "dx")
     _near(dz, want[3], low, 4, zn, "dz")
     _near(dh0, want[4], "f32", 2, 16.0, "dh0")
+
+
+@pytest.mark.parametrize("rows,cols", [(6, 40), (5, 200), (4, 512), (3, 1001), (2, 8192), (2, 9000)])
+@pytest.mark.parametrize("low", ["bf16", "f16", "f32"])
+def test_gate_gradients_of_a_join(rb, low, rows, cols):
+    """Branch, parameters and gradient of y' of one sign, no gradient of x: nothing cancels in dgate.  The gates of a row go over the whole
+    range, both signs."""
+    rng = np.random.default_rng(cols)
+    g = lambda *s: torch.from_numpy(rng.uniform(0.5, 1.5, s).astype(np.float32)).cuda()  # noqa: E731
+    z = np.resize(np.concatenate([GATES, [-v for v in GATES]]), (rows, cols))
+    y, b, gate, dy = g(rows, cols), g(rows, cols).to(LOW[low]), torch.from_numpy(z.astype(np.float32)).to(LOW[low]).cuda(), g(rows, cols)
+    w_post, scale = g(cols), g(cols)
+    j = rb.Join(alpha=0.5, eps=1e-5)
+    y2, _, rstd = rb.rampde_join_fwd(j, y, b, gate=gate, w_post=w_post, scale=scale, want_x=False, save_rstd=True)
+    got = rb.rampde_join_bwd(j, y2, b, rstd, dy, None, gate=gate, w_post=w_post, scale=scale).dgate
+    n = _np(b) / np.sqrt((_np(b) ** 2).mean(1, keepdims=True) + 1e-5)
+    want = 0.5 * _np(dy) * _np(scale) * n * _np(w_post) / (1 + np.exp(-z)) / (1 + np.exp(z))
+    # (the row's norm: a sum of squares in fp32, sqrt(cols) 2^-24)
+    _near(got, want, low, 1 + np.sqrt(cols) / 16, z, "dgate")
+
+
+def test_gate_gradients_of_closed_and_missing_gates(rb):
+    """Past the range of exp: s is 0, its derivative too, and a NaN shows"""
+    y, b, dy = torch.ones(1, 8, device="cuda"), torch.ones(1, 8, device="cuda"), torch.ones(1, 8, device="cuda")
+    gate = torch.tensor([[-87.0, -87.7, -88.5, -100.0, float("-inf"), 100.0, float("inf"), float("nan")]], device="cuda")
+    y2, _, rstd = rb.rampde_join_fwd(rb.Join(), y, b, gate=gate, want_x=False, save_rstd=True)
+    got = rb.rampde_join_bwd(rb.Join(), y2, b, rstd, dy, None, gate=gate).dgate[0]
+    assert (got[:7].abs() <= 2e-38).all() and torch.isnan(got[7])
