@@ -86,15 +86,29 @@ __device__ inline void store8(typename Elem<T>::S* p, int n, const float (&f)[8]
   }
 }
 
-// e = exp(-z) and s = 1 / (1 + e) on the hardware exp2 and reciprocal (relative error about 2e-7; s is 0 where e overflows).  1 - s is
-// e s, to as many places: by subtraction, that of an open gate has lost 12 of 24 at z = 8 and all of them at 17.
+// e = exp(-z) and s = 1 / (1 + e) on the hardware exp2 and reciprocal; s is 0 where e overflows.  1 - s is e s, to as many places: by
+// subtraction, that of an open gate has lost 12 of 24 at z = 8 and all of them at 17.
+//
+// Relative error about 2e-7, and that of the exponent's rounding, |z| 5e-8 (1e-6 at 20, 4e-6 at 80).  The latter is as if z were off by
+// half a unit in its last place, if z is fp32, and far less than that for z in 16 bits, which take it; fp32 operands, whose results are
+// held to 24 places, get what the product has dropped as a factor behind the exponential (in 16 bits six more instructions of some 35
+// an element).
 struct Gate {
   float e, s;
 };
+template <class T>
 __device__ inline Gate gate_of(float z) {
-  const float e = __builtin_amdgcn_exp2f(z * -1.44269504088896341f);
+  const float L = -1.44269504f, t = z * L;
+  float e = __builtin_amdgcn_exp2f(t);
+  if constexpr (sizeof(typename Elem<T>::S) == 4) {
+    const float dropped = fmaf(z, -1.92596299e-8f, fmaf(z, L, -t)), f = fmaf(e, dropped * 0.693147181f, e);  // (log2(e) in two parts)
+    e = fabsf(z) < 88.f ? f : e;  // (beyond, e or z may be infinite)
+  }
   return {e, __builtin_amdgcn_rcpf(1.f + e)};
 }
-__device__ inline float logistic(float z) { return gate_of(z).s; }
+template <class T>
+__device__ inline float logistic(float z) {
+  return gate_of<T>(z).s;
+}
 
 }  // namespace rampde

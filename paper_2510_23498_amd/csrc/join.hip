@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * W * R) void join_forward(JoinArgs g) {
             float gt[8];
             unpack8<T>(gr[j], gt);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sc[i] *= logistic(gt[i]);
+            for (int i = 0; i < 8; ++i) sc[i] *= logistic<T>(gt[i]);
           }
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(64 * W * R, sizeof(typename Elem<T>::S) == 2 ? 4 : 
           unpack8<T>(gr[j], gt);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const Gate v = gate_of(gt[i]);
+            const Gate v = gate_of<T>(gt[i]);
             const float gv = g.gate ? v.s : 1.f;
             nb[j][i] *= r_post;
             const float da = g.m.drop ? g.alpha * dv[j][i] * k[i] : g.alpha * dv[j][i];  // of s(gate) scale N(b) w_post

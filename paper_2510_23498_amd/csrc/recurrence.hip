@@ -368,8 +368,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(typename Elem<T>::S) == 2 && RE
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < kSeg; ++k) {
-      r[k][0] = logistic(Elem<T>::up(z[k][0]));
-      r[k][1] = SHARED ? r[k][0] : logistic(Elem<T>::up(z[k][1]));
+      r[k][0] = logistic<T>(Elem<T>::up(z[k][0]));
+      r[k][1] = SHARED ? r[k][0] : logistic<T>(Elem<T>::up(z[k][1]));
       in_order(k);
     }
   }
@@ -533,8 +533,8 @@ __global__ __launch_bounds__(64 * kWaves, REACH == kPairs ? 4 : 1) void recurren
     // (steps past the end of a sample come last: what they make of the state and of q is not used)
 #pragma unroll
     for (int k = 0; k < kSeg; ++k) {
-      r[k][0] = rate_of(gate_of(Elem<T>::up(z[k][0])));
-      r[k][1] = SHARED ? r[k][0] : rate_of(gate_of(Elem<T>::up(z[k][1])));
+      r[k][0] = rate_of(gate_of<T>(Elem<T>::up(z[k][0])));
+      r[k][1] = SHARED ? r[k][0] : rate_of(gate_of<T>(Elem<T>::up(z[k][1])));
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const float move = passed(r[k][i], Elem<T>::up(x[k][i]) - cur[i]);

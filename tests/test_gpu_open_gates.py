@@ -130,3 +130,18 @@ def test_gate_gradients_of_closed_and_missing_gates(rb):
     y2, _, rstd = rb.rampde_join_fwd(rb.Join(), y, b, gate=gate, want_x=False, save_rstd=True)
     got = rb.rampde_join_bwd(rb.Join(), y2, b, rstd, dy, None, gate=gate).dgate[0]
     assert (got[:7].abs() <= 2e-38).all() and torch.isnan(got[7])
+
+
+def test_gates_of_fp32_operands_over_their_whole_range(rb):
+    """Relative error that does not grow with |z|: one unit each of exponential and reciprocal (2^-23) and a handful of roundings, 8 of
+    2^-24 for s, 20 for products of s, 1 - s and two more factors.  (The reference forms s and 1 - s without subtractions.)"""
+    z = np.concatenate([np.linspace(-80, 80, 1281), np.linspace(-1, 1, 255)]).astype(np.float32).astype(np.float64)
+    s, c, D = 1 / (1 + np.exp(-z)), 1 / (1 + np.exp(z)), len(z)
+    zt, one = torch.from_numpy(z.astype(np.float32)).cuda(), torch.ones(1, 1, D, device="cuda")
+    h, hT, states = rb.rampde_recurrence_fwd(one, zt.view(1, 1, D), save_states=True)
+    dx, dz, dh0 = rb.rampde_recurrence_bwd(one, zt.view(1, 1, D), states, one, h0=torch.zeros(1, D, device="cuda"))
+    y, b = torch.zeros(1, D, device="cuda"), torch.ones(1, D, device="cuda")
+    y2, _, rstd = rb.rampde_join_fwd(rb.Join(eps=1e-30), y, b, gate=zt.view(1, D), want_x=False, save_rstd=True)
+    dgate = rb.rampde_join_bwd(rb.Join(eps=1e-30), y2, b, rstd, b, None, gate=zt.view(1, D)).dgate
+    for got, want, n in ((h, s, 8), (hT, s, 8), (dx, s, 8), (dh0, c, 8), (dz, s * c, 20), (y2, s, 12), (dgate, s * c, 20)):
+        assert np.max(np.abs(_np(got).ravel() / want - 1)) <= n * 2.0 ** -24
