@@ -364,7 +364,7 @@ int rampde_dropout(rampde_dtype low, int64_t n, const void *x, double p, uint64_
 typedef struct {
   int64_t rows, cols;        /* cols at most 16384 */
   rampde_dtype low;
-  double alpha, eps, p;      /* eps > 0 */
+  double alpha, eps, p;      /* as fp32: alpha finite, eps finite and > 0 */
   uint64_t seed, offset;     /* of the mask, see rampde_dropout */
   int64_t ld_b, ld_gate, ld_x; /* row pitch in elements of b, gate, x and of their gradients; 0: cols */
   int write_grads;           /* rampde_join_bwd: nonzero: dw_post, dscale and dw_pre are written, not accumulated into */

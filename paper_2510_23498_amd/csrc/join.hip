@@ -363,7 +363,9 @@ Mask mask_of(double p, uint64_t seed, uint64_t offset) {
 
 int check_join(const rampde_join* j, JoinArgs& g) {
   if (!j || j->rows < 1 || j->cols < 1 || !known_type(j->low)) return RAMPDE_EINVAL;
-  if (!(j->p >= 0.0 && j->p <= 1.0) || !(j->eps > 0.0) || !std::isfinite(j->eps) || !std::isfinite(j->alpha)) return RAMPDE_EINVAL;
+  g.alpha = (float)j->alpha;
+  g.eps = (float)j->eps;
+  if (!(j->p >= 0.0 && j->p <= 1.0) || !(g.eps > 0.f) || !std::isfinite(g.eps) || !std::isfinite(g.alpha)) return RAMPDE_EINVAL;  // (as fp32)
   if (j->cols > 16384) return RAMPDE_EUNSUPPORTED;
   const int64_t most = (int64_t)1 << 40;
   g.ld_b = j->ld_b ? j->ld_b : j->cols;
@@ -373,8 +375,6 @@ int check_join(const rampde_join* j, JoinArgs& g) {
   if (j->rows > ((int64_t)1 << 46) / std::max({g.ld_b, g.ld_gate, g.ld_x})) return RAMPDE_EUNSUPPORTED;  // (offsets fit 64 bits)
   g.rows = j->rows;
   g.cols = (int)j->cols;
-  g.alpha = (float)j->alpha;
-  g.eps = (float)j->eps;
   g.m = mask_of(j->p, j->seed, j->offset);
   return RAMPDE_OK;
 }
