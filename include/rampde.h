@@ -304,7 +304,9 @@ int rampde_odeint_bwd_tgrid(const rampde_velocity *vel, const float *theta, int6
  * status codes), with these differences: pointers need the alignment of their element type only (16 bytes and row pitches
  * in multiples of 16 bytes are faster; workspaces 256 bytes); the calls may be captured into a HIP graph; results do not
  * depend on timing (no floating-point atomics), two calls on the same inputs give the same bits.  Sums, states and
- * statistics are fp32.  Inputs that are NaN or infinite show in the outputs that depend on them. */
+ * statistics are fp32.  Inputs that are NaN or infinite show in the outputs that depend on them.  Every extent is at least 1
+ * (RAMPDE_EINVAL; there is nothing to do for an empty tensor); sizes that no launch takes, 2^32 threads along an axis, are
+ * RAMPDE_EUNSUPPORTED. */
 
 /* Gated linear recurrence along a sequence,
  *     h_t = h_{t-1} + r_t (x_t - h_{t-1}),   r_t = 1 / (1 + exp(-z_t)),   t = 0 .. T-1,   h_{-1} = h0,

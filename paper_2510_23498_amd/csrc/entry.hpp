@@ -17,6 +17,8 @@ __attribute__((visibility("hidden"))) int hip_fail(hipError_t e, const char* whe
 
 inline bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 inline bool known_type(rampde_dtype t) { return t == RAMPDE_F32 || t == RAMPDE_F16 || t == RAMPDE_BF16; }
+// a launch has less than 2^32 threads along an axis
+inline bool launchable(int64_t workgroups, int64_t threads) { return workgroups < ((int64_t)1 << 32) / threads; }
 inline size_t type_size(rampde_dtype t) { return t == RAMPDE_F32 ? 4 : 2; }
 
 }  // namespace rampde

@@ -719,7 +719,8 @@ int check_product(int64_t M, int64_t N, int64_t K, const void* a_values, const v
     return RAMPDE_EINVAL;
   p = fp8_plan(M, N, K);
   if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < product_space(M, N, p)) return RAMPDE_EWORKSPACE;
-  if (((M + 127) / 128) * ((N + 127) / 128) >= (int64_t)1 << 30) return RAMPDE_EUNSUPPORTED;
+  if (p.kind == kFewRows ? !launchable((N + 15) / 16, 64 * kFewWaves) : !launchable(((M + 255) / 256) * ((N + 255) / 256), 512))
+    return RAMPDE_EUNSUPPORTED;  // (small tiles are few)
   if (K >= (int64_t)1 << 23) return RAMPDE_EUNSUPPORTED;  // (offsets of a tile's rows fit 32 bits)
   g.a = (const uint8_t*)a_values, g.sa = (const uint8_t*)a_scales, g.b = (const uint8_t*)b_values, g.sb = (const uint8_t*)b_scales;
   g.c = C, g.M = M, g.N = N, g.ldc = ldc, g.accumulate = accumulate != 0;
@@ -768,7 +769,6 @@ int rampde_fp8_quantize(rampde_dtype src_type, rampde_fp8_mode mode, int64_t R, 
   if (ld < K || ld >= (int64_t)1 << 40 || ld > ((int64_t)1 << 46) / R || !aligned_to(src, e) || !aligned_to(values, 16) || !aligned_to(scales, 16) ||
       !aligned_to(values_t, 16) || !aligned_to(scales_t, 16))
     return RAMPDE_EINVAL;
-  if (R > (int64_t)65535 * 128 && mode != RAMPDE_FP8_ROWS) return RAMPDE_EUNSUPPORTED;  // (grid)
   QuantArgs g{};
   g.src = src, g.ld = ld, g.R = R, g.K = K;
   g.Kq = round_up(K, 128), g.Ks = round_up(g.Kq / 128, 4), g.Rq = round_up(R, 128), g.Rs = round_up(g.Rq / 128, 4);
@@ -776,13 +776,14 @@ int rampde_fp8_quantize(rampde_dtype src_type, rampde_fp8_mode mode, int64_t R, 
   if (mode == RAMPDE_FP8_COLS) g.values_t = g.values, g.scales_t = g.scales;
   const hipStream_t st = (hipStream_t)hip_stream;
   const dim3 row_grid((unsigned)((R + 15) / 16), (unsigned)((g.Kq / 128 + kRowBlocks - 1) / kRowBlocks));
-  if (row_grid.y > 65535) return RAMPDE_EUNSUPPORTED;
+  const dim3 grid((unsigned)(g.Kq / 128), (unsigned)(g.Rq / 128));
+  if (mode == RAMPDE_FP8_ROWS ? row_grid.y > 65535 || !launchable(row_grid.x, 256) : grid.y > 65535 || !launchable(grid.x, 512))
+    return RAMPDE_EUNSUPPORTED;
   return by_type(src_type, [&](auto tag) {
     typedef decltype(tag) T;
     if (mode == RAMPDE_FP8_ROWS) {
       quantize_rows<T><<<row_grid, 256, 0, st>>>(g);
     } else {
-      const dim3 grid((unsigned)(g.Kq / 128), (unsigned)(g.Rq / 128));
       // Four rows a thread, except for columns of 16 bits in many tiles: 16384 x 4096 in bf16 39 us with four rows, 33 with eight, of 1000 x
       // 1000 5.1 and 6.0; blocks 43 and 47, fp32 columns 64 and 65.
       const bool many = e == 2 && (int64_t)grid.x * grid.y >= 256;

@@ -651,13 +651,15 @@ bool fill_strides(const int64_t (&given)[2], int64_t B, int64_t T, int64_t width
   return B == 1 || T == 1 || s[0] >= (T - 1) * s[1] + width || s[1] >= (B - 1) * s[0] + width;
 }
 
+unsigned threads_of(int64_t T) { return 64 * (unsigned)std::min<int64_t>(kWaves, (T + kSeg - 1) / kSeg); }
+
 int check(const rampde_recurrence* r, RecArgs& g) {
   if (!r || r->B < 1 || r->T < 1 || r->D < 1 || !known_type(r->low)) return RAMPDE_EINVAL;
   if (r->share < 1 || (r->share & (r->share - 1)) || r->D % r->share) return RAMPDE_EINVAL;
   if (r->share > 128) return RAMPDE_EUNSUPPORTED;
   if (r->T >= (int64_t)1 << 30 || r->B >= (int64_t)1 << 31 || r->D >= (int64_t)1 << 31) return RAMPDE_EUNSUPPORTED;
   if (r->B * r->D > (int64_t)1 << 31) return RAMPDE_EUNSUPPORTED;
-  if ((r->B * r->D + kBlock - 1) / kBlock * ((r->T + kTile - 1) / kTile) >= (int64_t)1 << 31) return RAMPDE_EUNSUPPORTED;
+  if (!launchable((r->B * r->D + kBlock - 1) / kBlock * ((r->T + kTile - 1) / kTile), threads_of(r->T))) return RAMPDE_EUNSUPPORTED;
   g.T = r->T;
   g.D = (uint32_t)r->D;
   g.NC = (uint32_t)(r->B * r->D);
@@ -687,7 +689,7 @@ size_t chain_bytes(const RecArgs& g) {
 template <bool BACK, class T, int REACH>
 void launch_tile(const RecArgs& g, hipStream_t st) {
   const unsigned grid = g.blocks * (unsigned)g.tiles;
-  const unsigned threads = 64 * (unsigned)std::min<int64_t>(kWaves, (g.T + kSeg - 1) / kSeg);
+  const unsigned threads = threads_of(g.T);
   if constexpr (BACK) {
     if (g.share > 1) recurrence_bwd_tile<T, REACH, true><<<grid, threads, 0, st>>>(g);
     else recurrence_bwd_tile<T, REACH, false><<<grid, threads, 0, st>>>(g);

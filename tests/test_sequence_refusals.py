@@ -21,3 +21,21 @@ def test_join_parameters_that_fp32_does_not_hold(lib, bad):
     assert lib.rampde_join_workspace_bytes(j) == 0
     assert lib.rampde_join_fwd(j, *[P] * 9, None) == rb.EINVAL
     assert lib.rampde_join_bwd(j, *[P] * 16, 1 << 40, None) == rb.EINVAL
+
+
+def test_launches_of_more_threads_than_an_axis_has(lib):
+    """2^32 threads along the axis: refused as unsupported before the launch, not reported as an error of it"""
+    room = 1 << 60
+    q, m = lib.rampde_fp8_quantize, lib.rampde_fp8_matmul
+    assert q(rb.F32, 0, 1 << 28, 1, P, 0, P, P, None, None, None) == rb.EUNSUPPORTED          # 2^24 workgroups of 256
+    assert q(rb.F32, 0, 1, 1 << 26, P, 0, P, P, None, None, None) == rb.EUNSUPPORTED          # (the other axis: 65535 workgroups)
+    for mode, t in ((1, None), (2, P)):
+        assert q(rb.F32, mode, 1, 1 << 30, P, 0, P, P, t, t, None) == rb.EUNSUPPORTED         # 2^23 workgroups of 512
+        assert q(rb.F32, mode, 1 << 23, 1, P, 0, P, P, t, t, None) == rb.EUNSUPPORTED
+    assert m(4, 1 << 26, 1, P, P, P, P, rb.F32, 0, P, 0, P, room, None) == rb.EUNSUPPORTED    # 2^22 workgroups of 1024
+    assert m(1 << 20, 1 << 20, 1, P, P, P, P, rb.F32, 0, P, 0, P, room, None) == rb.EUNSUPPORTED
+    r = rb._Recurrence(1 << 10, 1 << 11, 1 << 17, 1, rb.BF16)                                 # 2^20 blocks, 16 tiles each, of 512
+    assert lib.rampde_recurrence_workspace_bytes(C.byref(r)) == 0
+    assert lib.rampde_recurrence_fwd(C.byref(r), P, P, P, P, P, P, P, P, room, None) == rb.EUNSUPPORTED
+    r = rb._Recurrence(1 << 10, 1, 1 << 17, 1, rb.BF16)                                       # (as many samples of one step fit)
+    assert lib.rampde_recurrence_workspace_bytes(C.byref(r)) == 256
