@@ -253,15 +253,27 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
-def _stream_ptr(stream):
+def _stream_of(stream, device):
+    """Handle of `stream`, or of the current one of the tensors' GPU"""
+    # (without an object around the current stream's handle, which takes a fifth of the time of a small call)
     if stream is None:
-        stream = torch.cuda.current_stream()
-    return C.c_void_p(stream.cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    if stream.device != device:
+        raise ValueError(f"stream: on {stream.device}, the tensors are on {device}")
+    return stream.cuda_stream
 
 
-def _check_dev(t: torch.Tensor, dtype, numel, name):
-    if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.numel() == numel):
-        raise ValueError(f"{name}: need a contiguous cuda tensor of {dtype} with {numel} elements, "
+def _on(device, fn, *args) -> int:
+    """fn on the tensors' GPU.  The library launches on the current one, and every GPU's default stream has the handle 0."""
+    if device.index == torch._C._cuda_getDevice():
+        return fn(*args)
+    with torch.cuda.device(device):
+        return fn(*args)
+
+
+def _check_dev(t: torch.Tensor, dtype, numel, name, device=None):
+    if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.numel() == numel and device in (None, t.device)):
+        raise ValueError(f"{name}: need a contiguous cuda tensor of {dtype} with {numel} elements{f' on {device}' if device else ''}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
@@ -311,21 +323,20 @@ def rampde_odeint_fwd(vel: Velocity, theta: torch.Tensor, y0: torch.Tensor, tgri
     B = int(y0.shape[0])
     tg = np.ascontiguousarray(np.asarray(tgrid, dtype=np.float64))
     N = int(tg.shape[0]) - 1
-    P = rampde_num_params(vel)
-    _check_dev(theta, torch.float32, P, "theta")
+    P, device = rampde_num_params(vel), y0.device
+    _check_dev(theta, torch.float32, P, "theta", device)
     _check_dev(y0, torch.float32, B * vel.d, "y0")
     if ckpt is None:
         ckpt = torch.empty(vel.ckpt_shape(B, N), dtype=pol.torch_low, device=y0.device)
     if yN is None:
         yN = torch.empty_like(y0)
-    _check_dev(ckpt, pol.torch_low, (N + 1) * B * vel.d, "ckpt")
-    _check_dev(yN, torch.float32, B * vel.d, "yN")
+    _check_dev(ckpt, pol.torch_low, (N + 1) * B * vel.d, "ckpt", device)
+    _check_dev(yN, torch.float32, B * vel.d, "yN", device)
     if workspace is None:
         workspace = alloc_workspace(vel, B, N, tab, pol, False, y0.device)
     pc = pol.c
-    rc = lib.rampde_odeint_fwd(C.byref(vel.c), _ptr(theta), _ptr(y0), B, tg.ctypes.data_as(C.POINTER(C.c_double)), N,
-                               C.byref(tab.c), C.byref(pc), _ptr(ckpt), _ptr(yN), _ptr(workspace),
-                               workspace.numel(), _stream_ptr(stream))
+    rc = _on(device, lib.rampde_odeint_fwd, C.byref(vel.c), _ptr(theta), _ptr(y0), B, tg.ctypes.data_as(C.POINTER(C.c_double)), N,
+             C.byref(tab.c), C.byref(pc), _ptr(ckpt), _ptr(yN), _ptr(workspace), workspace.numel(), _stream_of(stream, device))
     if rc != OK:
         raise RampdeError(rc, rampde_strerror(rc))
     return yN, ckpt
@@ -343,14 +354,15 @@ def rampde_odeint_fwd_static(vel: Velocity, theta: torch.Tensor, y0: torch.Tenso
     B = int(y0.shape[0])
     tg = np.ascontiguousarray(np.asarray(tgrid, dtype=np.float64))
     N = int(tg.shape[0]) - 1
-    _check_dev(theta, torch.float32, rampde_num_params(vel), "theta")
+    device = y0.device
+    _check_dev(theta, torch.float32, rampde_num_params(vel), "theta", device)
     _check_dev(y0, torch.float32, B * vel.d, "y0")
-    _check_dev(ckpt, pol.torch_low, (N + 1) * B * vel.d, "ckpt")
-    _check_dev(yN, torch.float32, B * vel.d, "yN")
+    _check_dev(ckpt, pol.torch_low, (N + 1) * B * vel.d, "ckpt", device)
+    _check_dev(yN, torch.float32, B * vel.d, "yN", device)
     pc = pol.c
-    rc = lib.rampde_odeint_fwd_static(C.byref(vel.c), _ptr(theta), _ptr(y0), B,
-                                      tg.ctypes.data_as(C.POINTER(C.c_double)), N, C.byref(tab.c), C.byref(pc),
-                                      _ptr(ckpt), _ptr(yN), _stream_ptr(stream))
+    rc = _on(device, lib.rampde_odeint_fwd_static, C.byref(vel.c), _ptr(theta), _ptr(y0), B,
+             tg.ctypes.data_as(C.POINTER(C.c_double)), N, C.byref(tab.c), C.byref(pc), _ptr(ckpt), _ptr(yN),
+             _stream_of(stream, device))
     if rc != OK:
         raise RampdeError(rc, rampde_strerror(rc))
     return yN, ckpt
@@ -370,18 +382,18 @@ def rampde_odeint_bwd(vel: Velocity, theta: torch.Tensor, tgrid, tab: Tableau, p
     B = int(grad_yN.shape[0])
     tg = np.ascontiguousarray(np.asarray(tgrid, dtype=np.float64))
     N = int(tg.shape[0]) - 1
-    P = rampde_num_params(vel)
-    _check_dev(theta, torch.float32, P, "theta")
+    P, device = rampde_num_params(vel), grad_yN.device
+    _check_dev(theta, torch.float32, P, "theta", device)
     _check_dev(grad_yN, torch.float32, B * vel.d, "grad_yN")
-    _check_dev(ckpt, pol.torch_low, (N + 1) * B * vel.d, "ckpt")
+    _check_dev(ckpt, pol.torch_low, (N + 1) * B * vel.d, "ckpt", device)
     if grad_ys is not None:
-        _check_dev(grad_ys, torch.float32, (N + 1) * B * vel.d, "grad_ys")
+        _check_dev(grad_ys, torch.float32, (N + 1) * B * vel.d, "grad_ys", device)
     if grad_y0 is None:
         grad_y0 = torch.empty_like(grad_yN)
     if grad_theta is None:
         grad_theta = torch.zeros(P, dtype=torch.float32, device=grad_yN.device)
-    _check_dev(grad_y0, torch.float32, B * vel.d, "grad_y0")
-    _check_dev(grad_theta, torch.float32, P, "grad_theta")
+    _check_dev(grad_y0, torch.float32, B * vel.d, "grad_y0", device)
+    _check_dev(grad_theta, torch.float32, P, "grad_theta", device)
     if workspace is None:
         workspace = alloc_workspace(vel, B, N, tab, pol, True, grad_yN.device)
     pc = pol.c
@@ -393,16 +405,14 @@ def rampde_odeint_bwd(vel: Velocity, theta: torch.Tensor, tgrid, tab: Tableau, p
     hist_p = hist.ctypes.data_as(C.POINTER(C.c_float)) if want_info else None
     stats_p = C.byref(stats) if want_info else None
     if grad_t is not None:
-        _check_dev(grad_t, torch.float32, N + 1, "grad_t")
-        rc = lib.rampde_odeint_bwd_tgrid(C.byref(vel.c), _ptr(theta), B, tg.ctypes.data_as(C.POINTER(C.c_double)), N,
-                                         C.byref(tab.c), C.byref(pc), _ptr(ckpt), _ptr(grad_yN), _ptr(grad_ys),
-                                         _ptr(grad_y0), _ptr(grad_theta), _ptr(grad_t), hist_p, stats_p,
-                                         _ptr(workspace), workspace.numel(), _stream_ptr(stream))
+        _check_dev(grad_t, torch.float32, N + 1, "grad_t", device)
+        rc = _on(device, lib.rampde_odeint_bwd_tgrid, C.byref(vel.c), _ptr(theta), B, tg.ctypes.data_as(C.POINTER(C.c_double)),
+                 N, C.byref(tab.c), C.byref(pc), _ptr(ckpt), _ptr(grad_yN), _ptr(grad_ys), _ptr(grad_y0), _ptr(grad_theta),
+                 _ptr(grad_t), hist_p, stats_p, _ptr(workspace), workspace.numel(), _stream_of(stream, device))
     else:
-        rc = lib.rampde_odeint_bwd(C.byref(vel.c), _ptr(theta), B, tg.ctypes.data_as(C.POINTER(C.c_double)), N,
-                                   C.byref(tab.c), C.byref(pc), _ptr(ckpt), _ptr(grad_yN), _ptr(grad_ys),
-                                   _ptr(grad_y0), _ptr(grad_theta), hist_p, stats_p, _ptr(workspace),
-                                   workspace.numel(), _stream_ptr(stream))
+        rc = _on(device, lib.rampde_odeint_bwd, C.byref(vel.c), _ptr(theta), B, tg.ctypes.data_as(C.POINTER(C.c_double)), N,
+                 C.byref(tab.c), C.byref(pc), _ptr(ckpt), _ptr(grad_yN), _ptr(grad_ys), _ptr(grad_y0), _ptr(grad_theta),
+                 hist_p, stats_p, _ptr(workspace), workspace.numel(), _stream_of(stream, device))
     info = None
     if want_info:
         info = BwdInfo(stats.status, stats.failed_step, stats.retries, stats.s_first, stats.s_last, stats.s_min,
@@ -432,11 +442,6 @@ def _raise(rc: int) -> None:
 
 def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
-
-
-def _stream_of(stream, device):
-    # (the current stream's handle without an object around it: a fifth of the time of a small call otherwise)
-    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
 def _type_of(t: torch.Tensor, name: str) -> int:
@@ -556,8 +561,8 @@ def rampde_recurrence_fwd(x: torch.Tensor, z: torch.Tensor, h0: Optional[torch.T
         states = _new(stream, torch.empty, n, dtype=torch.float32, device=device)
     _check_like(lengths, torch.int32, state[:1], device, "lengths")
     workspace = _space(nbytes, workspace, device, stream)
-    _raise(_lib.rampde_recurrence_fwd(ref, _at(x), _at(z), _at(h0), _at(lengths), _at(h), _at(hT), _at(states),
-                                      _at(workspace), _size(workspace), _stream_of(stream, device)))
+    _raise(_on(device, _lib.rampde_recurrence_fwd, ref, _at(x), _at(z), _at(h0), _at(lengths), _at(h), _at(hT), _at(states),
+               _at(workspace), _size(workspace), _stream_of(stream, device)))
     return h, hT, states
 
 
@@ -588,8 +593,8 @@ def rampde_recurrence_bwd(x: torch.Tensor, z: torch.Tensor, states: torch.Tensor
         dh0 = _new(stream, torch.empty, state, dtype=torch.float32, device=device)
     _check_like(dh0, torch.float32, state, device, "dh0")
     workspace = _space(nbytes, workspace, device, stream)
-    _raise(_lib.rampde_recurrence_bwd(ref, _at(x), _at(z), _at(lengths), _at(states), _at(dh), _at(dhT), _at(dx), _at(dz),
-                                      _at(dh0), _at(workspace), _size(workspace), _stream_of(stream, device)))
+    _raise(_on(device, _lib.rampde_recurrence_bwd, ref, _at(x), _at(z), _at(lengths), _at(states), _at(dh), _at(dhT), _at(dx),
+               _at(dz), _at(dh0), _at(workspace), _size(workspace), _stream_of(stream, device)))
     return dx, dz, dh0
 
 
@@ -602,7 +607,7 @@ def rampde_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, out: O
         out = _empty_like(stream, x)
     else:
         _check_like(out, x.dtype, x.shape, device, "out")
-    _raise(load_library().rampde_dropout(low, x.numel(), _at(x), p, seed, offset, _at(out), _stream_of(stream, device)))
+    _raise(_on(device, load_library().rampde_dropout, low, x.numel(), _at(x), p, seed, offset, _at(out), _stream_of(stream, device)))
     return out
 
 
@@ -668,8 +673,8 @@ def rampde_join_fwd(join: Join, y: torch.Tensor, b: Optional[torch.Tensor] = Non
         _check_like(rstd, torch.float32, (2, y.shape[0]), device, "rstd")
     elif save_rstd:
         rstd = _new(stream, torch.empty, (2, y.shape[0]), dtype=torch.float32, device=device)
-    _raise(load_library().rampde_join_fwd(C.byref(j), _at(y), _at(b), _at(gate), _at(w_post), _at(scale), _at(w_pre), _at(y_out),
-                                          _at(x), _at(rstd), _stream_of(stream, device)))
+    _raise(_on(device, load_library().rampde_join_fwd, C.byref(j), _at(y), _at(b), _at(gate), _at(w_post), _at(scale), _at(w_pre),
+               _at(y_out), _at(x), _at(rstd), _stream_of(stream, device)))
     return (y if b is None else y_out), x, rstd
 
 
@@ -713,9 +718,9 @@ def rampde_join_bwd(join: Join, y_out: torch.Tensor, b: Optional[torch.Tensor], 
                                for w, d, n in zip((w_post, scale, w_pre), (dw_post, dscale, dw_pre), new)]
     db, dgate = (_like_of(stream, d, t, name) for d, t, name in ((db, b, "db"), (dgate, gate, "dgate")))
     workspace = _space(_needed(int(lib.rampde_join_workspace_bytes(C.byref(j)))), workspace, device, stream)
-    _raise(lib.rampde_join_bwd(C.byref(j), _at(y_out), _at(b), _at(gate), _at(w_post), _at(scale), _at(w_pre), _at(rstd),
-                               _at(dy_out), _at(dx), _at(dy), _at(db), _at(dgate), _at(dw_post), _at(dscale), _at(dw_pre),
-                               _at(workspace), _size(workspace), _stream_of(stream, device)))
+    _raise(_on(device, lib.rampde_join_bwd, C.byref(j), _at(y_out), _at(b), _at(gate), _at(w_post), _at(scale), _at(w_pre),
+               _at(rstd), _at(dy_out), _at(dx), _at(dy), _at(db), _at(dgate), _at(dw_post), _at(dscale), _at(dw_pre),
+               _at(workspace), _size(workspace), _stream_of(stream, device)))
     return JoinGrads(dy, db, dgate, dw_post, dscale, dw_pre)
 
 
@@ -798,7 +803,8 @@ def rampde_fp8_quantize(src: torch.Tensor, mode: str = "rows", out: Optional[Fp8
     elif shape_t is None or (out_t.rows, out_t.cols) != shape_t[:2] or out_t.device != device:
         raise ValueError(f"out_t: need {'no operand' if shape_t is None else f'an operand of shape {shape_t[:2]} on {device}'}")
     t_values, t_scales = (None, None) if out_t is None else out_t._at
-    _raise(_lib.rampde_fp8_quantize(low, code, R, K, src.data_ptr(), ld, *out._at, t_values, t_scales, _stream_of(stream, device)))
+    _raise(_on(device, _lib.rampde_fp8_quantize, low, code, R, K, src.data_ptr(), ld, *out._at, t_values, t_scales,
+               _stream_of(stream, device)))
     return out if out_t is None else (out, out_t)
 
 
@@ -828,7 +834,7 @@ def rampde_fp8_matmul(a: Fp8, b: Fp8, dtype=torch.bfloat16, out: Optional[torch.
     if short_sums:
         if accumulate or c_type == F32:
             raise ValueError("short_sums: results of 16 bits, not accumulated")
-        _raise(_lib.rampde_fp8_matmul_short(M, N, K, *a._at, *b._at, c_type, _at(out), ldc, at, size, st))
+        _raise(_on(device, _lib.rampde_fp8_matmul_short, M, N, K, *a._at, *b._at, c_type, _at(out), ldc, at, size, st))
     else:
-        _raise(_lib.rampde_fp8_matmul(M, N, K, *a._at, *b._at, c_type, 1 if accumulate else 0, _at(out), ldc, at, size, st))
+        _raise(_on(device, _lib.rampde_fp8_matmul, M, N, K, *a._at, *b._at, c_type, 1 if accumulate else 0, _at(out), ldc, at, size, st))
     return out
