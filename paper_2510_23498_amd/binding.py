@@ -500,9 +500,11 @@ def _size(t: torch.Tensor) -> int:
     return t.numel() * t.element_size()
 
 
-def _needed(nbytes: int) -> int:
+def _needed(nbytes: int, call=None, ref=None) -> int:
+    """Bytes of workspace; a query that gives none has rejected the arguments, for the reason that `call` without buffers names"""
     if nbytes == 0:
-        raise RampdeError(EINVAL, "workspace query rejected the arguments")
+        rc = EINVAL if call is None else call(ref, *[0] * (len(call.argtypes) - 1))
+        raise RampdeError(rc, f"the arguments are rejected: {rampde_strerror(rc)}")
     return nbytes
 
 
@@ -518,10 +520,14 @@ def _recurrence_plan(dtype, x_shape, x_stride, z_shape, z_stride, h_stride):
                          "divides the number of channels")
     if not (_rows_apart(x_shape, x_stride) and _rows_apart(z_shape, z_stride)):
         raise ValueError(f"x and z: channels have to be neighbours and rows apart, got strides {x_stride} and {z_stride}")
-    r = _Recurrence(B, T, D, D // gates, _TYPES[dtype], x_stride[:2], z_stride[:2], h_stride[:2] if h_stride else (0, 0))
+    share = D // gates
+    if share & (share - 1) or share > 128:
+        raise RampdeError(EUNSUPPORTED, f"{share} channels share a gate (x {tuple(x_shape)}, z {tuple(z_shape)}): need a power of two, "
+                          "at most 128")
+    r = _Recurrence(B, T, D, share, _TYPES[dtype], x_stride[:2], z_stride[:2], h_stride[:2] if h_stride else (0, 0))
     ref = C.byref(r)
     lib = load_library()
-    nbytes = _needed(int(lib.rampde_recurrence_workspace_bytes(ref)))
+    nbytes = _needed(int(lib.rampde_recurrence_workspace_bytes(ref)), lib.rampde_recurrence_fwd, ref)
     return ref, int(lib.rampde_recurrence_states(ref)), 0 if nbytes == 256 else nbytes
 
 
@@ -538,7 +544,7 @@ def rampde_recurrence_fwd(x: torch.Tensor, z: torch.Tensor, h0: Optional[torch.T
                           save_states: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
     """Gated linear recurrence h_t = h_{t-1} + sigmoid(z_t) (x_t - h_{t-1}).
 
-    x [B, T, D] and z [B, T, D / share] may be slices (channels neighbouring); h0 [B, D] fp32; lengths [B] int32.  Returns
+    x [B, T, D] and z [B, T, D / share] (share a power of two up to 128) may be slices (channels neighbouring); h0 [B, D] fp32; lengths [B] int32.  Returns
     (h, hT, states): states is None unless given or `save_states`, which the backward pass needs.  Asynchronous.
     """
     device = x.device
@@ -680,8 +686,12 @@ def rampde_join_fwd(join: Join, y: torch.Tensor, b: Optional[torch.Tensor] = Non
 
 def _like_of(stream, grad, t, name):
     """The gradient's tensor: as given, or one like its input's"""
-    if t is None or grad is None:
-        return None if t is None else _empty_like(stream, t)
+    if t is None:
+        if grad is not None:
+            raise ValueError(f"{name}: there is no input that it would be the gradient of")
+        return None
+    if grad is None:
+        return _empty_like(stream, t)
     _check_like(grad, t.dtype, t.shape, t.device, name, contiguous=False)
     if t.shape[0] > 1 and grad.stride(0) != t.stride(0):
         raise ValueError(f"{name}: row pitch {grad.stride(0)} is not that of its input, {t.stride(0)}")
@@ -717,7 +727,7 @@ def rampde_join_bwd(join: Join, y_out: torch.Tensor, b: Optional[torch.Tensor], 
     dw_post, dscale, dw_pre = [(n if d is None else d) if w is not None or d is not None else None
                                for w, d, n in zip((w_post, scale, w_pre), (dw_post, dscale, dw_pre), new)]
     db, dgate = (_like_of(stream, d, t, name) for d, t, name in ((db, b, "db"), (dgate, gate, "dgate")))
-    workspace = _space(_needed(int(lib.rampde_join_workspace_bytes(C.byref(j)))), workspace, device, stream)
+    workspace = _space(_needed(int(lib.rampde_join_workspace_bytes(C.byref(j))), lib.rampde_join_fwd, C.byref(j)), workspace, device, stream)
     _raise(_on(device, lib.rampde_join_bwd, C.byref(j), _at(y_out), _at(b), _at(gate), _at(w_post), _at(scale), _at(w_pre),
                _at(rstd), _at(dy_out), _at(dx), _at(dy), _at(db), _at(dgate), _at(dw_post), _at(dscale), _at(dw_pre),
                _at(workspace), _size(workspace), _stream_of(stream, device)))
@@ -784,7 +794,9 @@ def _quantize_plan(shape, stride, mode):
 
     def sizes(rows, cols):
         return rows, cols, int(lib.rampde_fp8_value_bytes(rows, cols)), int(lib.rampde_fp8_scale_bytes(rows, cols))
-    code = _FP8_MODES[mode]
+    code = _FP8_MODES.get(mode)
+    if code is None:
+        raise ValueError(f"mode: need one of {', '.join(_FP8_MODES)}, got {mode!r}")
     return code, R, K, stride[0] if R > 1 else 0, sizes(K, R) if code == 1 else sizes(R, K), sizes(K, R) if code == 2 else None
 
 

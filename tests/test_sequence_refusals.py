@@ -39,3 +39,33 @@ def test_launches_of_more_threads_than_an_axis_has(lib):
     assert lib.rampde_recurrence_fwd(C.byref(r), P, P, P, P, P, P, P, P, room, None) == rb.EUNSUPPORTED
     r = rb._Recurrence(1 << 10, 1, 1 << 17, 1, rb.BF16)                                       # (as many samples of one step fit)
     assert lib.rampde_recurrence_workspace_bytes(C.byref(r)) == 256
+
+
+@pytest.mark.parametrize("D,gates", [(6, 2), (96, 2), (80, 1), (256, 1)])
+def test_gates_of_other_numbers_of_channels_say_so(D, gates):
+    torch = pytest.importorskip("torch")
+    with pytest.raises(rb.RampdeError, match="power of two, at most 128") as e:
+        rb._recurrence_plan(torch.bfloat16, (2, 3, D), (3 * D, D, 1), (2, 3, gates), (3 * gates, gates, 1), None)
+    assert e.value.code == rb.EUNSUPPORTED
+
+
+def test_rejected_arguments_come_with_the_reason():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(rb.RampdeError) as e:   # (steps past 2^30)
+        rb._recurrence_plan(torch.bfloat16, (1, 1 << 31, 2), (1 << 32, 2, 1), (1, 1 << 31, 2), (1 << 32, 2, 1), None)
+    assert e.value.code == rb.EUNSUPPORTED
+    lib = rb.load_library()
+    for kw, code in ((dict(cols=16385), rb.EUNSUPPORTED), (dict(cols=0), rb.EINVAL)):
+        j = C.byref(rb._Join(4, kw["cols"], rb.BF16, 1.0, 1e-6))
+        with pytest.raises(rb.RampdeError) as e:
+            rb._needed(int(lib.rampde_join_workspace_bytes(j)), lib.rampde_join_fwd, j)
+        assert e.value.code == code
+
+
+def test_unknown_modes_and_gradients_of_nothing():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError, match="rows, cols, blocks"):
+        rb._quantize_plan((2, 3), (3, 1), "diagonal")
+    with pytest.raises(ValueError, match="dgate"):
+        rb._like_of(None, torch.zeros(2, 3), None, "dgate")
+    assert rb._like_of(None, None, None, "dgate") is None
