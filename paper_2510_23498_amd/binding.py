@@ -541,15 +541,17 @@ def _recurrence(x: torch.Tensor, z: torch.Tensor, h: Optional[torch.Tensor]):
 def rampde_recurrence_fwd(x: torch.Tensor, z: torch.Tensor, h0: Optional[torch.Tensor] = None,
                           lengths: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None,
                           hT: Optional[torch.Tensor] = None, states: Optional[torch.Tensor] = None,
-                          save_states: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
+                          save_states: bool = False, workspace: Optional[torch.Tensor] = None, stream=None, want_h: bool = True):
     """Gated linear recurrence h_t = h_{t-1} + sigmoid(z_t) (x_t - h_{t-1}).
 
-    x [B, T, D] and z [B, T, D / share] (share a power of two up to 128) may be slices (channels neighbouring); h0 [B, D] fp32; lengths [B] int32.  Returns
-    (h, hT, states): states is None unless given or `save_states`, which the backward pass needs.  Asynchronous.
+    x [B, T, D] and z [B, T, D / share] (share a power of two up to 128) may be slices (channels neighbouring); h0 [B, D] fp32;
+    lengths [B] int32.  Returns (h, hT, states): states is None unless given or `save_states`, which the backward pass needs; h is
+    None where neither it is given nor `want_h` (the last state alone is of interest, a third of the traffic less).  Asynchronous.
     """
     device = x.device
     if h is None:
-        h = _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format)
+        if want_h:
+            h = _new(stream, torch.empty_like, x, memory_format=torch.contiguous_format)
     else:
         _check_like(h, x.dtype, x.shape, device, "h", contiguous=False)
     ref, n, nbytes = _recurrence(x, z, h)

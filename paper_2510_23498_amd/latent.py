@@ -86,7 +86,7 @@ class Encoder:
             self.saved.append((y, rstd, u, z, gate, b, before))
         x = rb.rampde_dropout(x, p, seed, offset=(len(self.into) + 1) << 40) if p else x
         u, z, _ = self._split(self.head.forward(x), B)
-        _, st["head"], before = rb.rampde_recurrence_fwd(u, z, h0=st.get("head"), lengths=lengths, save_states=train)
+        _, st["head"], before = rb.rampde_recurrence_fwd(u, z, h0=st.get("head"), lengths=lengths, save_states=train, want_h=False)
         self.tail = (u, z, before, lengths, seed, p)
         return st["head"]
 

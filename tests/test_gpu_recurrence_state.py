@@ -46,3 +46,16 @@ def test_state_and_its_gradient_in_place(rb, B, T, D, share, low):
         assert again[2] is grad
         for a, b in zip(again, back):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("B,T,D,share,low", [(4, 1, 96, 1, "bf16"), (3, 70, 33, 1, "f16"), (2, 900, 256, 64, "f32")])
+def test_last_state_alone(rb, B, T, D, share, low):
+    """Without h, the other outputs have the same bits; a given h is written all the same"""
+    rng = np.random.default_rng(T)
+    x, z = _normal(rng, (B, T, D), LOW[low]), _normal(rng, (B, T, D // share), LOW[low])
+    n = torch.tensor([T, 0, T // 2, T][:B], dtype=torch.int32, device="cuda")
+    h, hT, states = rb.rampde_recurrence_fwd(x, z, lengths=n, save_states=True)
+    none, hT2, states2 = rb.rampde_recurrence_fwd(x, z, lengths=n, save_states=True, want_h=False)
+    assert none is None and torch.equal(hT, hT2) and torch.equal(states, states2)
+    out = torch.zeros_like(h)
+    assert rb.rampde_recurrence_fwd(x, z, lengths=n, h=out, want_h=False)[0] is out and torch.equal(out, h)
