@@ -27,10 +27,11 @@ class Linear:
     def __init__(self, n_out: int, n_in: int, generator, device):
         self.w = torch.randn(n_out, n_in, generator=generator, device=device) * n_in ** -0.5
         self.grad = torch.zeros_like(self.w)
+        self.wq, self.wt = rb.Fp8.empty(n_out, n_in, self.w.device), rb.Fp8.empty(n_in, n_out, self.w.device)
         self.quantise()
 
     def quantise(self):
-        self.wq, self.wt = rb.rampde_fp8_quantize(self.w, "blocks")
+        rb.rampde_fp8_quantize(self.w, "blocks", out=self.wq, out_t=self.wt)
 
     def forward(self, x: torch.Tensor, dtype=LOW) -> torch.Tensor:
         self.x = x
