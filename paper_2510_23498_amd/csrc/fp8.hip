@@ -1,9 +1,10 @@
 // Matrix product in 8-bit floating point with a power-of-two scale for every 128 values along the contraction
 // (rampde_fp8_quantize, rampde_fp8_matmul, rampde_fp8_matmul_short).
 //
-// Sums in fp32 (rampde_fp8_matmul, any result): every e4m3 value times its scale is a bf16 number, one instruction converts two of
+// Sums in fp32 (rampde_fp8_matmul, any result): an e4m3 value times its scale is a bf16 number, one instruction converts two of
 // them, and 16-bit matrix instructions form exact products and fp32 sums (5e-9 relative on blocks of 128 normally distributed values
-// against 64 bits, 8e-8 on values spread over all exponents).
+// against 64 bits, 8e-8 on values spread over all exponents).  That is so for scales of 2^-124 to 2^119; with others the smallest values
+// are below bf16's (e4m3 goes down to 2^-9, bf16 to 2^-133) or the largest above, and the wavefronts that meet one take short sums.
 //
 // Short sums (rampde_fp8_matmul_short, results of 16 bits; a caller has to ask for them): gfx950's scaled matrix instructions multiply
 // the 8-bit values and apply an exponent per operand row and 32 values, so that a scale that is a power of two costs nothing, at twice
@@ -275,6 +276,11 @@ __device__ inline u16x8 to_bf16(int lo, int hi, float scale) {
   return __builtin_bit_cast(u16x8, r);
 }
 __device__ inline float scale_value(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+// Whether bf16 does not hold some e4m3 value times one of these four scales: below 2^-124 (byte 3) the smallest values, above 2^119 (246)
+// the largest.  A byte below n is one that borrows in x - n without having had its upper bit itself.
+__device__ inline bool any_extreme(uint32_t bytes) {
+  return ((((bytes - 0x03030303u) & ~bytes) | ((~bytes - 0x09090909u) & bytes)) & 0x80808080u) != 0;
+}
 
 template <class T>
 __device__ inline void put_c(const Fp8Args& g, int64_t m, int64_t n, f32x4 v) {
@@ -314,42 +320,50 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_rows(Fp8Args g) {
     qa[i] = g.sa + m * g.Ks;
   }
   f32x4 acc[FM];
-#pragma unroll
-  for (int i = 0; i < FM; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int first = (int)blockIdx.y * g.split_blocks, end = first + g.split_blocks < g.nb ? first + g.split_blocks : g.nb;
   const int per = (end - first + kFewWaves - 1) / kFewWaves, k0 = first + wave * per, k1 = k0 + per < end ? k0 + per : end;
-  for (int k = k0; k < k1; k += AHEAD) {
-    i32x8 fa[AHEAD][FM], fb[AHEAD];
-    int sa[AHEAD][FM], sb[AHEAD];
+  bool extreme = false;  // (of this lane)
+  auto sum = [&](auto short_c) {
+    constexpr bool NOW_SHORT = decltype(short_c)::value;
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int at = k + u < k1 ? k + u : k;
-      fb[u] = *reinterpret_cast<const i32x8*>(pb + (int64_t)at * 128);
-      sb[u] = qb[at];
+    for (int i = 0; i < FM; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = k0; k < k1; k += AHEAD) {
+      i32x8 fa[AHEAD][FM], fb[AHEAD];
+      int sa[AHEAD][FM], sb[AHEAD];
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        fa[u][i] = *reinterpret_cast<const i32x8*>(pa[i] + (int64_t)at * 128);
-        sa[u][i] = qa[i][at];
+      for (int u = 0; u < AHEAD; ++u) {
+        const int at = k + u < k1 ? k + u : k;
+        fb[u] = *reinterpret_cast<const i32x8*>(pb + (int64_t)at * 128);
+        sb[u] = qb[at];
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          fa[u][i] = *reinterpret_cast<const i32x8*>(pa[i] + (int64_t)at * 128);
+          sa[u][i] = qa[i][at];
+        }
       }
-    }
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      if (k + u >= k1) break;
-      if constexpr (!SHORT) {
+      for (int u = 0; u < AHEAD; ++u) {
+        if (k + u >= k1) break;
+        if constexpr (!NOW_SHORT) {
+          static_assert(FM <= 2, "bytes of a word");
+          extreme |= any_extreme((uint32_t)sb[u] | (uint32_t)sa[u][0] << 8 | (uint32_t)sa[u][FM - 1] << 16 | 127u << 24);
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          const u16x8 wb = to_bf16(fb[u][2 * h], fb[u][2 * h + 1], scale_value(sb[u]));
+          for (int h = 0; h < 4; ++h) {
+            const u16x8 wb = to_bf16(fb[u][2 * h], fb[u][2 * h + 1], scale_value(sb[u]));
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+              acc[i] = Low<BF16>::mfma16(wb, to_bf16(fa[u][i][2 * h], fa[u][i][2 * h + 1], scale_value(sa[u][i])), acc[i]);
+          }
+        } else {
 #pragma unroll
           for (int i = 0; i < FM; ++i)
-            acc[i] = Low<BF16>::mfma16(wb, to_bf16(fa[u][i][2 * h], fa[u][i][2 * h + 1], scale_value(sa[u][i])), acc[i]);
+            acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u][i], acc[i], 0, 0, 0, sb[u], 0, sa[u][i]);
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-          acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u][i], acc[i], 0, 0, 0, sb[u], 0, sa[u][i]);
       }
     }
-  }
+  };
+  sum(std::integral_constant<bool, SHORT>{});
+  if (!SHORT && __any(extreme)) sum(std::true_type{});
 #pragma unroll
   for (int i = 0; i < FM; ++i) sums[wave][i][lane] = acc[i];
   __syncthreads();
@@ -532,6 +546,7 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp
     __builtin_amdgcn_sched_barrier(0);
   };
   i32x8 fa[2][FM], fb[2][FN];
+  bool extreme = false;  // (of this lane)
   load_scales(0);
   issue(0);
   issue(1);
@@ -551,6 +566,12 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp
         for (int a = 0; a < FM; ++a) sa[a] = sa_next[a];
 #pragma unroll
         for (int b = 0; b < FN; ++b) sb[b] = sb_next[b];
+      }
+      if constexpr (!SHORT) {
+#pragma unroll
+        for (int a = 0; a < FM; ++a) extreme |= any_extreme(sa[a]);
+#pragma unroll
+        for (int b = 0; b < FN; ++b) extreme |= any_extreme(sb[b]);
       }
       load_scales((kb >> 2) + 1);
     }
@@ -573,6 +594,37 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp
   }
   __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0), lgkmcnt(0): the end's extra loads and reads
   __builtin_amdgcn_s_barrier();
+  // Scales that bf16 has no room for (see any_extreme): a wavefront that has met one sums its blocks of C once more, straight from memory
+  // and with the scaled instructions.  That is rare and may be slow; the loop above must not know of it (with both kinds of instructions in it,
+  // or with itself a second time behind it, it spills: 2000 and 263 us instead of 211 for 16384 x 4096 x 2048).
+  if (!SHORT && __any(extreme)) {
+#pragma unroll
+    for (int a = 0; a < FM; ++a)
+#pragma unroll
+      for (int b = 0; b < FN; ++b)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[a][b][q] = 0.f;
+#pragma unroll 1
+    for (int64_t at = (int64_t)kb0 * 128; at < (int64_t)kb1 * 128; at += 64) {  // half a block, of which a lane has 32 bytes
+      auto load = [&](const uint8_t* v, const uint8_t* q, int64_t row0, int64_t rows, i32x8& f, int& scale) {
+        const int64_t row = row0 + frow < rows ? row0 + frow : rows - 1;
+        f = *reinterpret_cast<const i32x8*>(v + row * g.Kq + at + half * 32);
+        scale = q[row * g.Ks + (at >> 7)];
+      };
+      i32x8 w[FN];
+      int sw[FN];
+#pragma unroll
+      for (int b = 0; b < FN; ++b) load(g.b, g.sb, n0 + (wn * FN + b) * 32, g.N, w[b], sw[b]);
+#pragma unroll
+      for (int a = 0; a < FM; ++a) {
+        i32x8 v;
+        int sv;
+        load(g.a, g.sa, m0 + (wm * FM + a) * 32, g.M, v, sv);
+#pragma unroll
+        for (int b = 0; b < FN; ++b) acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[b], v, acc[a][b], 0, 0, 0, sw[b], 0, sv);
+      }
+    }
+  }
 
   // ---- accumulator layout of a block: row of C = lane % 32, column = 8 (q / 4) + 4 (lane / 32) + q % 4
   if (g.splits > 1) {

@@ -124,3 +124,55 @@ def test_short_sums_of_fp32_results_are_refused(rb):
     for kw in (dict(dtype=torch.float32), dict(out=torch.zeros(4, 5, device="cuda"), accumulate=True)):
         with pytest.raises(ValueError):
             rb.rampde_fp8_matmul(a, b, short_sums=True, **kw)
+
+
+@pytest.mark.parametrize("low", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("M,N", [(16, 40), (29, 70), (127, 20), (300, 200), (2100, 4100)])
+def test_scales_at_both_ends_of_their_range(rb, low, M, N):
+    """Every scale that a block can have, against one that brings the product back to about 1: two products of 4 x 4 places a result, whose
+    sum is exact where fp32 holds it, and off by a unit of the larger product's last place where they are further apart.  Few rows,
+    small and large tiles, either operand."""
+    rng = np.random.default_rng(M)
+    every = torch.arange(127, dtype=torch.uint8)   # all finite values from 0 up
+
+    def operand(rows, scales, values):
+        v = torch.zeros(rows, 256, dtype=torch.uint8)
+        v[:, 3], v[:, 200] = values, values.flip(0)
+        s = torch.full((rows, 4), 127, dtype=torch.uint8)
+        s[:, 0], s[:, 1] = scales, scales
+        return rb.Fp8(v.cuda(), s.cuda(), 256)
+    for scale in (0, 1, 2, 3, 4, 60, 244, 246, 247, 248, 254):
+        a = torch.full((M,), 127, dtype=torch.uint8)
+        a[rng.integers(0, M, max(1, M // 40))] = scale   # (a few rows of many)
+        b = torch.full((N,), 127, dtype=torch.uint8)
+        b[rng.integers(0, N, max(1, N // 40))] = 254 - scale
+        va, vb = every[torch.arange(M) % 127], every[(torch.arange(N) * 5 + 64) % 127]
+        x, y = operand(M, a, va), operand(N, b, vb)
+        for p, q in ((x, y), (y, x)):
+            d = [t.values.view(torch.float8_e4m3fn).double()[:, [3, 200]] * torch.exp2(t.scales[:, :1].double() - 127) for t in (p, q)]
+            want = d[0] @ d[1].T
+            keep = want.abs() < 2.0 ** 127   # (infinite, or on the way there, otherwise)
+            got = rb.rampde_fp8_matmul(p, q, dtype=LOW[low])
+            top = (d[0][:, :1] * d[1][:, 0]).abs().maximum((d[0][:, 1:] * d[1][:, 1]).abs())
+            exact = keep & ((low != "f32") | (want.float().double() == want))
+            assert torch.equal(got[exact], want.float().to(LOW[low])[exact]), scale
+            assert ((got.double() - want).abs() <= 2.0 ** -23 * top)[keep & ~exact].all(), scale
+            if low != "f32":
+                assert torch.equal(rb.rampde_fp8_matmul(p, q, dtype=LOW[low], short_sums=True)[keep], got[keep]), scale
+        assert not torch.isnan(rb.rampde_fp8_matmul(x, y, dtype=LOW[low])).any()
+
+
+def test_rows_of_the_smallest_and_largest_numbers(rb):
+    """Quantised from fp32: rows of 2^-135 and of 3.4e38 (which rounds to 2^128) against columns that bring them back"""
+    x = torch.zeros(40, 130, device="cuda")
+    x[:, 0], x[:, 129] = 1.0, 1.0
+    x[3, 0], x[3, 129], x[17, 0], x[17, 129] = 2.0 ** -135, 2.0 ** -134, 3.4e38, 3.4e38
+    w = torch.zeros(50, 130, device="cuda")
+    w[:, 0], w[:, 129] = 1.0, 2.0
+    w[5, 0], w[6, 0] = 2.0 ** 120, 2.0 ** -120
+    got = rb.rampde_fp8_matmul(rb.rampde_fp8_quantize(x), rb.rampde_fp8_quantize(w), dtype=torch.float32)
+    assert got[3, 5] == 2.0 ** -15 + 2.0 ** -133 and got[17, 6] == float("inf") and got[0, 5] == 2.0 ** 120
+    assert got[3, 0] == 2.0 ** -135 + 2.0 ** -133 and (got[[0, 1, 2, 4, 39]][:, :5] == 3.0).all()
+    w[:, 129] = 0
+    got = rb.rampde_fp8_matmul(rb.rampde_fp8_quantize(x), rb.rampde_fp8_quantize(w), dtype=torch.float32)
+    assert got[17, 6] == 2.0 ** 8 and got[17, 0] == float("inf") and got[17, 5] == float("inf")
