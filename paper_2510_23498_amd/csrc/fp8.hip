@@ -391,12 +391,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_rows(Fp8Args g) {
 // has the time of a whole one to arrive.
 //
 // 256 x 256 on 8 wavefronts (2 x 4, each 128 x 64).  Sums in fp32 are bound by the 16-bit matrix instructions and the conversions in
-// front of them: bf16 results 16384 x 4096 x 2048 211 us and 16384 x 2048 x 4096 203 us, fp32 results 4096 x 2048 x 16384 224 to 275 us by
-// card and heat (1.0 to 1.35 of the 1.8 PFLOP/s that these instructions reach by themselves).  Short sums: per block of 128, reading
-// fragments from LDS takes as many cycles as the matrix instructions (about 2000 at their full rates), and the chip's power lets matrix
-// instructions on such data run at 3.2 to 3.7 PFLOP/s (5 on constant data); the same two products 122 to 151 and 119 to 154 us (1.8 to
-// 2.3 PFLOP/s).  Tried and slower or no faster: 4 wavefronts of 128 x 128, rings of 3 to 5 half-size slots, tiles of 256 x 128, the 16 x 16
-// instructions (15 % faster by themselves, but their fragments spill here), wave priorities, conversions a group ahead.
+// front of them: bf16 results 16384 x 4096 x 2048 211 to 222 us and 16384 x 2048 x 4096 203 to 217 us by card and heat (1.25 to 1.35 of
+// the 1.8 PFLOP/s that these instructions reach by themselves); 128 x 128 tiles, fp32 results 4096 x 2048 x 16384 219 to 280 us.  Short
+// sums: per block of 128, reading fragments from LDS takes as many cycles as the matrix instructions (about 2000 at their full rates), and
+// the chip's power lets matrix instructions on such data run at 3.2 to 3.7 PFLOP/s (5 on constant data); the first two products 119 to 151
+// and 119 to 154 us (1.8 to 2.3 PFLOP/s).  Tried and slower or no faster, on short sums: 4 wavefronts of 128 x 128, rings of 3 to 5
+// half-size slots, tiles of 256 x 128, the 16 x 16 instructions (15 % faster by themselves, but their fragments spill here), wave
+// priorities; on fp32 sums: conversions a group ahead.
 template <int WM, int WN, int FM, int FN>
 struct Fp8Tile {
   static constexpr int TM = 32 * WM * FM, TN = 32 * WN * FN, WAVES = WM * WN;
@@ -729,16 +730,22 @@ Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K) {
     return Fp8Plan{kind, (nb + per - 1) / per, per};
   };
   const int64_t small = ((M + 127) / 128) * ((N + 127) / 128);
-  // Up to 32 rows: tiles of 128 rows take 9 to 11 us however few of the rows there are, few-row workgroups 3 to 8 us (M = 16: 3 / 5 us
-  // at 512 x 512, 8 / 11 us at 4096 x 4096) and fall behind only where the contraction is long and the columns fill the chip as well
-  // (M = 16: 24 / 19 us at N = 4096, K = 16384).  Columns that leave compute units idle: the contraction in pieces of at least one block
-  // per wavefront (M = 16, N = 1024, K = 8192: 12.8 us whole, 8 us in four pieces; N = 64, K = 16384: 23 and 7.8 us).
+  // (Times of fp32 sums, bf16 results; short sums in brackets where they differ.)
+  // Up to 32 rows: tiles of 128 rows take 13 us (10) however few of the rows there are, few-row workgroups 3 to 11 us (M = 16: 3.2 against
+  // 6.7 (5.3) us at 512 x 512, 8.4 against 13.9 (11) at 4096 x 4096; M = 32: 11 against 14 (11)).  They fall behind only where the contraction is
+  // long and the columns fill the chip as well (M = 16, N = 4096, K = 16384: 24.3 against 23.4 (20)).  Columns that leave compute units
+  // idle: the contraction in pieces of at least one block per wavefront (M = 16, N = 1024, K = 8192: 13 us whole, 8 us in four pieces;
+  // N = 64, K = 16384: 23 and 7.7 us).
   if (M <= 32) return pieces(kFewRows, std::max<int64_t>(1, std::min<int64_t>(256 / ((N + 15) / 16), nb / 16)));
   // More tiles of 128 x 128 than are resident at two per compute unit: tiles of 256 x 256, which read their operands half as often
-  // (4096^3: 64 us, small tiles 86; 2304 x 4096 x 4096: 60 and 64; but 2048 x 4096 x 4096: 54, small tiles 42).
+  // (4096^3: 101 (59) us, small tiles 120 (74); 16384 x 4096 x 2048: 213 (119) and 231 (148); 2304 x 4096 x 4096: 86 (53) and 84 (60)); with no
+  // more, small ones (2048 x 4096 x 4096: 63 (41) us, large tiles 86 (53); 4096 x 2048 x 16384: 216 to 229 and 296).  One large tile occupies a
+  // compute unit, and where the last round of them leaves most units idle they lose all the same: 4352 x 4096 x 4096, 272 tiles, 174 (103) us,
+  // small tiles 134 to 138 (90); 8448 x 4096 x 2048 140 and 123.
   if (small > 512) return pieces(kLargeTiles, 1);
   // Few small tiles: the contraction in pieces of at least 8 blocks, as long as there is at most one workgroup per compute unit (with up
-  // to two: 2048^3 30 us instead of 15, 1024 x 4096 x 4096 37 instead of 29; without pieces 128 x 1024 x 8192 takes 40 us, with 14).
+  // to two: 2048^3 36 (32) us instead of 21 (15), 1024 x 4096 x 4096 49 (39) instead of 38 (30); without pieces 128 x 1024 x 8192 takes 57 (39) us,
+  // with 17 (14), 512 x 512 x 4096 31 (22) and 17 (14)).
   return pieces(kSmallTiles, std::max<int64_t>(1, std::min<int64_t>({256 / small, nb / 8, 16})));
 }
 
