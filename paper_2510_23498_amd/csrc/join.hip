@@ -12,8 +12,8 @@
 // gate, dy', dx in, dy, db, dgate out).  Measured on 16384 x 2048 in bf16 with gate and dropout: forward 91 us (5.2 TB/s), backward 149 us
 // (5.0 TB/s) and 5 us to fold the column sums; a plain copy of that size reaches 5.05 TB/s.  Columns in no multiple of eight cost
 // accesses across cache lines, and draws of two blocks of the generator for eight elements: 16384 x 1001 47 us forward, 1024 columns 40.
-// Beyond 8192 columns the backward pass has twice the columns in a lane and spills: 1.9 TB/s at 1024 x 16384.  Few rows are bound by
-// latency: 16 x 2048 4.7 us, 1003 x 1001 in f16 8 us forward and 12 + 4 us backward.
+// Beyond 8192 columns the backward pass has twice the columns in a lane and spills: 236 us (1.6 TB/s) at 1024 x 16384.  Few rows are
+// bound by latency: 16 x 2048 4.7 us, 1003 x 1001 in f16 8 us forward and 11 + 5 us backward.
 #include <algorithm>
 #include <cmath>
 #include "entry.hpp"

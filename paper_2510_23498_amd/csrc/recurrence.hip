@@ -10,9 +10,10 @@
 // so steps are split between workgroups: 128 channels and 128 steps each, one pass over the data, and what goes from tile to tile is
 // 8 bytes per channel.  States are saved every 16 steps (fp32, an eighth of h in 16 bits) for the backward pass, which recomputes the
 // others.  Measured in bf16, kernels alone: 8 x 4096 x 2048 forward 88 us (402 MB + 17 of states: 4.8 TB/s), backward 133 us
-// (671 + 17 MB: 5.2 TB/s); 1 x 65536 x 1024 98 and 139 us; a plain copy of that size reaches 5.0 TB/s.  The words between the tiles
+// (671 + 17 MB: 5.2 TB/s); 1 x 65536 x 1024 100 and 144 us; a plain copy of that size reaches 5.0 TB/s.  The words between the tiles
 // are emptied before (5 us there, 2 us for 7 x 1003 x 1024).  Few tiles are bound by latency: 7 x 1003 x 1024 in f16, gates shared
-// by 64, 12 and 19 us for 31 and 45 MB; one step of 32 x 2048 4.6 us.
+// by 64, 12 and 19.5 us for 31 and 45 MB; one step of 32 x 2048 4.4 us.  Odd channels, whose accesses are 2 bytes wide: 8 x 4096 x 2047
+// 136 and 273 us.
 #include <algorithm>
 #include <type_traits>
 #include "entry.hpp"
