@@ -421,8 +421,7 @@ int rampde_fp8_quantize(rampde_dtype src_type, rampde_fp8_mode mode, int64_t R, 
                         void *values, void *scales, void *values_t, void *scales_t, void *hip_stream);
 
 /* C[M][N] = A B^T, or C += A B^T (fp32 C only), of two quantised operands with K < 2^23 columns: fp32 sums of exact products,
- * rounded once.  (Results whose tile meets a scale below 2^-124 or above 2^119 have the short sums that are described below: no
- * 16-bit number holds such values.)
+ * rounded once.  (Results whose tile meets a scale above 2^116 or passes 2^122 have the short sums that are described below.)
  *   c_type, ldc   type and row pitch (0: N) of C
  *   workspace     dev, rampde_fp8_workspace_bytes(M, N, K): partial sums where few blocks of C share a long contraction (256
  *                 bytes: none of it is used) */

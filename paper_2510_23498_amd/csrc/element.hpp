@@ -91,8 +91,8 @@ __device__ inline void store8(typename Elem<T>::S* p, int n, const float (&f)[8]
 //
 // Relative error about 2e-7, and that of the exponent's rounding, |z| 5e-8 (1e-6 at 20, 4e-6 at 80).  The latter is as if z were off by
 // half a unit in its last place, if z is fp32, and far less than that for z in 16 bits, which take it; fp32 operands, whose results are
-// held to 24 places, get what the product has dropped as a factor behind the exponential (in 16 bits six more instructions of some 35
-// an element).
+// held to 24 places, get what the product has dropped as a factor behind the exponential: six instructions of some 40 an element (4 x
+// 4096 x 2048 in fp32 87.2 instead of 86.3 us forward, join of 65536 x 64 17.3 instead of 16.4).
 struct Gate {
   float e, s;
 };

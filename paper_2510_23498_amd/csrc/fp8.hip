@@ -3,8 +3,9 @@
 //
 // Sums in fp32 (rampde_fp8_matmul, any result): an e4m3 value times its scale is a bf16 number, one instruction converts two of
 // them, and 16-bit matrix instructions form exact products and fp32 sums (5e-9 relative on blocks of 128 normally distributed values
-// against 64 bits, 8e-8 on values spread over all exponents).  That is so for scales of 2^-124 to 2^119; with others the smallest values
-// are below bf16's (e4m3 goes down to 2^-9, bf16 to 2^-133) or the largest above, and the wavefronts that meet one take short sums.
+// against 64 bits, 8e-8 on values spread over all exponents).  e4m3 goes down to 2^-9, scales to 2^-127 and bf16 to 2^-133 only (gradients
+// that die away along a sequence do get there): operands are converted with three more in the exponent, and the sums take it back.
+// Values past 2^124 and sums past 2^122, which then have no room above, take short sums.
 //
 // Short sums (rampde_fp8_matmul_short, results of 16 bits; a caller has to ask for them): gfx950's scaled matrix instructions multiply
 // the 8-bit values and apply an exponent per operand row and 32 values, so that a scale that is a power of two costs nothing, at twice
@@ -276,11 +277,11 @@ __device__ inline u16x8 to_bf16(int lo, int hi, float scale) {
   return __builtin_bit_cast(u16x8, r);
 }
 __device__ inline float scale_value(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
-// Whether bf16 does not hold some e4m3 value times one of these four scales: below 2^-124 (byte 3) the smallest values, above 2^119 (246)
-// the largest.  A byte below n is one that borrows in x - n without having had its upper bit itself.
-__device__ inline bool any_extreme(uint32_t bytes) {
-  return ((((bytes - 0x03030303u) & ~bytes) | ((~bytes - 0x09090909u) & bytes)) & 0x80808080u) != 0;
-}
+// With kOffset more in the exponent, bf16 holds every e4m3 value (448 at the most) times a scale of up to 2^116 (byte 243).  Whether one of
+// these four is larger: a byte of x below n is one that borrows in x - n without having had its upper bit itself.
+constexpr uint32_t kOffset = 3;
+constexpr float kTakeBack = 1.f / (1 << 2 * kOffset);
+__device__ inline bool any_above(uint32_t bytes) { return ((~bytes - 0x0C0C0C0Cu) & bytes & 0x80808080u) != 0; }
 
 template <class T>
 __device__ inline void put_c(const Fp8Args& g, int64_t m, int64_t n, f32x4 v) {
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_rows(Fp8Args g) {
   f32x4 acc[FM];
   const int first = (int)blockIdx.y * g.split_blocks, end = first + g.split_blocks < g.nb ? first + g.split_blocks : g.nb;
   const int per = (end - first + kFewWaves - 1) / kFewWaves, k0 = first + wave * per, k1 = k0 + per < end ? k0 + per : end;
-  bool extreme = false;  // (of this lane)
+  bool above = false;  // (a scale that this lane has met)
   auto sum = [&](auto short_c) {
     constexpr bool NOW_SHORT = decltype(short_c)::value;
 #pragma unroll
@@ -346,13 +347,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_rows(Fp8Args g) {
         if (k + u >= k1) break;
         if constexpr (!NOW_SHORT) {
           static_assert(FM <= 2, "bytes of a word");
-          extreme |= any_extreme((uint32_t)sb[u] | (uint32_t)sa[u][0] << 8 | (uint32_t)sa[u][FM - 1] << 16 | 127u << 24);
+          above |= any_above((uint32_t)sb[u] | (uint32_t)sa[u][0] << 8 | (uint32_t)sa[u][FM - 1] << 16);
 #pragma unroll
           for (int h = 0; h < 4; ++h) {
-            const u16x8 wb = to_bf16(fb[u][2 * h], fb[u][2 * h + 1], scale_value(sb[u]));
+            const u16x8 wb = to_bf16(fb[u][2 * h], fb[u][2 * h + 1], scale_value(sb[u] + kOffset));
 #pragma unroll
             for (int i = 0; i < FM; ++i)
-              acc[i] = Low<BF16>::mfma16(wb, to_bf16(fa[u][i][2 * h], fa[u][i][2 * h + 1], scale_value(sa[u][i])), acc[i]);
+              acc[i] = Low<BF16>::mfma16(wb, to_bf16(fa[u][i][2 * h], fa[u][i][2 * h + 1], scale_value(sa[u][i] + kOffset)), acc[i]);
           }
         } else {
 #pragma unroll
@@ -363,7 +364,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_rows(Fp8Args g) {
     }
   };
   sum(std::integral_constant<bool, SHORT>{});
-  if (!SHORT && __any(extreme)) sum(std::true_type{});
+  if constexpr (!SHORT) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(acc[i][e]));
+    if (__any(above || top == INFINITY)) {
+      sum(std::true_type{});
+    } else {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) acc[i] *= kTakeBack;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < FM; ++i) sums[wave][i][lane] = acc[i];
   __syncthreads();
@@ -391,7 +404,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_rows(Fp8Args g) {
 // has the time of a whole one to arrive.
 //
 // 256 x 256 on 8 wavefronts (2 x 4, each 128 x 64).  Sums in fp32 are bound by the 16-bit matrix instructions and the conversions in
-// front of them: bf16 results 16384 x 4096 x 2048 211 to 222 us and 16384 x 2048 x 4096 203 to 217 us by card and heat (1.25 to 1.35 of
+// front of them: bf16 results 16384 x 4096 x 2048 213 to 255 us and 16384 x 2048 x 4096 205 to 221 us by card and heat (1.1 to 1.35 of
 // the 1.8 PFLOP/s that these instructions reach by themselves); 128 x 128 tiles, fp32 results 4096 x 2048 x 16384 219 to 280 us.  Short
 // sums: per block of 128, reading fragments from LDS takes as many cycles as the matrix instructions (about 2000 at their full rates), and
 // the chip's power lets matrix instructions on such data run at 3.2 to 3.7 PFLOP/s (5 on constant data); the first two products 119 to 151
@@ -547,7 +560,7 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp
     __builtin_amdgcn_sched_barrier(0);
   };
   i32x8 fa[2][FM], fb[2][FN];
-  bool extreme = false;  // (of this lane)
+  bool above = false;  // (a scale that this lane has met)
   load_scales(0);
   issue(0);
   issue(1);
@@ -570,9 +583,14 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp
       }
       if constexpr (!SHORT) {
 #pragma unroll
-        for (int a = 0; a < FM; ++a) extreme |= any_extreme(sa[a]);
+        for (int a = 0; a < FM; ++a) above |= any_above(sa[a]);
 #pragma unroll
-        for (int b = 0; b < FN; ++b) extreme |= any_extreme(sb[b]);
+        for (int b = 0; b < FN; ++b) above |= any_above(sb[b]);
+        // (to four bytes at a time; a byte that carries is one that is above)
+#pragma unroll
+        for (int a = 0; a < FM; ++a) sa[a] += kOffset * 0x01010101u;
+#pragma unroll
+        for (int b = 0; b < FN; ++b) sb[b] += kOffset * 0x01010101u;
       }
       load_scales((kb >> 2) + 1);
     }
@@ -595,10 +613,26 @@ __global__ __launch_bounds__(64 * WM * WN, FM * FN > 8 ? 1 : 2) void fp8_tile(Fp
   }
   __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0), lgkmcnt(0): the end's extra loads and reads
   __builtin_amdgcn_s_barrier();
-  // Scales that bf16 has no room for (see any_extreme): a wavefront that has met one sums its blocks of C once more, straight from memory
-  // and with the scaled instructions.  That is rare and may be slow; the loop above must not know of it (with both kinds of instructions in it,
-  // or with itself a second time behind it, it spills: 2000 and 263 us instead of 211 for 16384 x 4096 x 2048).
-  if (!SHORT && __any(extreme)) {
+  // What the offset leaves no room for (see any_above; NaN are none of it): the wavefront sums its blocks of C once more, straight from
+  // memory and with the scaled instructions.  That is rare and may be slow; the loop above must not know of it (with both kinds of
+  // instructions in it, or with itself a second time behind it, it spills: 2000 and 263 us instead of 211 for 16384 x 4096 x 2048).
+  if constexpr (!SHORT) {
+    float top = 0.f;
+#pragma unroll
+    for (int a = 0; a < FM; ++a)
+#pragma unroll
+      for (int b = 0; b < FN; ++b)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) top = fmaxf(top, fabsf(acc[a][b][q]));
+    above = __any(above || top == INFINITY);
+#pragma unroll
+    for (int a = 0; a < FM; ++a)
+#pragma unroll
+      for (int b = 0; b < FN; ++b)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[a][b][q] *= kTakeBack;
+  }
+  if (!SHORT && above) {
 #pragma unroll
     for (int a = 0; a < FM; ++a)
 #pragma unroll

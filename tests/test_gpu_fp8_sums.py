@@ -176,3 +176,23 @@ def test_rows_of_the_smallest_and_largest_numbers(rb):
     w[:, 129] = 0
     got = rb.rampde_fp8_matmul(rb.rampde_fp8_quantize(x), rb.rampde_fp8_quantize(w), dtype=torch.float32)
     assert got[17, 6] == 2.0 ** 8 and got[17, 0] == float("inf") and got[17, 5] == float("inf")
+
+
+@pytest.mark.parametrize("M,N", [(16, 40), (29, 70), (300, 200), (2100, 4100)])
+def test_sums_up_to_the_largest_number(rb, M, N):
+    """One product of ones against powers of two, up to 2^127, and sums past it"""
+    x, w = torch.zeros(M, 256, device="cuda"), torch.zeros(N, 256, device="cuda")
+    x[:, 7], x[:, 250] = 1.0, 1.0
+    e = torch.arange(N, device="cuda") % 16 + 112.0   # 2^112 to 2^127
+    w[:, 7] = torch.exp2(e)
+    got = rb.rampde_fp8_matmul(rb.rampde_fp8_quantize(x), rb.rampde_fp8_quantize(w), dtype=torch.float32)
+    assert (got == torch.exp2(e)).all()
+    w[:, 250] = w[:, 7]
+    got = rb.rampde_fp8_matmul(rb.rampde_fp8_quantize(x), rb.rampde_fp8_quantize(w), dtype=torch.bfloat16)
+    assert (got.float() == torch.exp2(e + 1)).all()   # (infinite for 2^128)
+    w[:, 250] = -w[:, 7]
+    got = rb.rampde_fp8_matmul(rb.rampde_fp8_quantize(x), rb.rampde_fp8_quantize(w), dtype=torch.float32)
+    assert (got == 0).all()
+    x[3, 9] = float("nan")
+    got = rb.rampde_fp8_matmul(rb.rampde_fp8_quantize(x), rb.rampde_fp8_quantize(w), dtype=torch.float32)
+    assert torch.isnan(got[3]).all() and (got[[i for i in range(M) if i != 3]] == 0).all()
